@@ -1,8 +1,10 @@
 """Python binding of the 0/1 Adam hot-path library (``libzoadam.so``).
 
 Argument marshalling only: every step of the optimizer runs in the HIP
-kernels behind the C ABI declared in ``include/zo_adam.h``.  Functions keep
-the C names (``zo_adam_init``, ``zo_local_step``, ...); ``ZoAdam`` wraps a
+kernels behind the C ABI declared in ``include/zo_adam.h``; the operators that
+stand next to it (``include/zo_ops.h``: 4-bit matrices and their products, top
+logits, the distillation loss) are in ``operators.py`` and are imported here
+too.  Functions keep the C names (``zo_adam_init``, ``zo_local_step``, ...); ``ZoAdam`` wraps a
 handle for convenience.  Device buffers are torch tensors (PyTorch provides
 device memory and streams only).  There is no fallback: if the library is not
 built, every call raises.
@@ -29,6 +31,9 @@ EXPORTS = (
     "zo_strerror", "zo_last_hip_error", "zo_diag_divsqrt", "zo_diag_copy", "zo_diag_stream",
     "zo_diag_server_pattern",
     "zo_config_check", "zo_plan_num_chunks", "zo_plan_chunks",
+    "zo_mx4_code_bytes", "zo_mx4_scale_bytes", "zo_mx4_quantize", "zo_mx4_dequantize",
+    "zo_mx4_product", "zo_mx4_linear", "zo_top_logits_ws", "zo_top_logits", "zo_distill_ws",
+    "zo_distill_loss", "zo_ops_last_hip_error",
 )
 
 
@@ -54,6 +59,22 @@ class _Config(ctypes.Structure):
 
 class _State(ctypes.Structure):
     _fields_ = [(k, ctypes.c_void_p) for k in ("x", "m", "v", "u", "err", "srv_err", "anchor")]
+
+
+class _Mx4(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
+
+
+class _Distill(ctypes.Structure):
+    _fields_ = [("z", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("vocab", ctypes.c_int64), ("ldz", ctypes.c_int64), ("top", ctypes.c_int32),
+                ("values", ctypes.c_void_p), ("columns", ctypes.c_void_p),
+                ("teacher_lse", ctypes.c_void_p), ("labels", ctypes.c_void_p),
+                ("row_weight", ctypes.c_void_p), ("tau", ctypes.c_float),
+                ("kd_weight", ctypes.c_float), ("ce_weight", ctypes.c_float),
+                ("loss", ctypes.c_void_p), ("dz", ctypes.c_void_p), ("lddz", ctypes.c_int64),
+                ("ws", ctypes.c_void_p), ("ws_bytes", ctypes.c_int64)]
 
 
 _lib = None
@@ -102,6 +123,17 @@ def lib():
             "zo_config_check": ([ctypes.POINTER(_Config)], ci),
             "zo_plan_num_chunks": ([i32, vp, i32], i64),
             "zo_plan_chunks": ([i32, vp, i32, vp, vp, vp], i64),
+            "zo_mx4_code_bytes": ([i64, i64], i64),
+            "zo_mx4_scale_bytes": ([i64, i64], i64),
+            "zo_mx4_quantize": ([vp, i32, i64, i64, i64, vp, vp, vp], ci),
+            "zo_mx4_dequantize": ([vp, vp, i32, i64, vp], ci),
+            "zo_mx4_product": ([vp, vp, vp, i32, i64, vp], ci),
+            "zo_mx4_linear": ([vp, i32, i64, vp, vp, vp, i32, i64, vp], ci),
+            "zo_top_logits_ws": ([i64, i64, i32], i64),
+            "zo_top_logits": ([vp, i32, i64, i64, i64, i32, f32, vp, vp, vp, vp, i64, vp], ci),
+            "zo_distill_ws": ([i64, i64], i64),
+            "zo_distill_loss": ([ctypes.POINTER(_Distill), vp], ci),
+            "zo_ops_last_hip_error": ([], ctypes.c_char_p),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
@@ -477,3 +509,8 @@ class ZoAdam:
         if rc != ZO_OK:
             raise ZoError(rc, "zo_inexact_chunks")
         return c.value
+
+
+from .operators import (Mx4, zo_distill_loss, zo_distill_ws, zo_mx4_code_bytes,  # noqa: E402
+                        zo_mx4_dequantize, zo_mx4_linear, zo_mx4_product, zo_mx4_quantize,
+                        zo_mx4_scale_bytes, zo_top_logits, zo_top_logits_ws)

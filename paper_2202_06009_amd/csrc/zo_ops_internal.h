@@ -1,0 +1,39 @@
+// zo_ops_internal.h -- launchers of the operators of zo_ops.h, called by its
+// host side after every argument has been checked.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "zo_ops.h"
+
+namespace zo {
+
+// An mx4 matrix as the kernels take it: KT = ceil(cols / 128) tiles of 128
+// columns.
+struct Mx4View {
+    uint8_t *codes, *scales;
+    int64_t rows, cols, kt;
+};
+
+hipError_t launch_mx4_quantize(const void *x, int gt, int64_t rows, int64_t cols, int64_t ld,
+                               const Mx4View *q, const Mx4View *qt, hipStream_t st);
+hipError_t launch_mx4_dequantize(const Mx4View &q, void *out, int gt, int64_t ld,
+                                 hipStream_t st);
+hipError_t launch_mx4_product(const Mx4View &a, const Mx4View &b, void *out, int gt, int64_t ld,
+                              hipStream_t st);
+
+struct TopArgs {
+    const void *z;
+    int64_t rows, vocab, ld;
+    int top;
+    float tau;
+    float *values;
+    int32_t *columns;
+    float *lse;
+    void *ws;
+};
+hipError_t launch_top_logits(const TopArgs &a, int gt, hipStream_t st);
+hipError_t launch_distill(const zo_distill &a, hipStream_t st);
+
+}  // namespace zo

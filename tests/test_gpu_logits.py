@@ -1,0 +1,403 @@
+"""Top logits and the distillation loss on the GPU against the 64-bit oracle."""
+import numpy as np
+import pytest
+
+import operators_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+HALF_ULP = {"float32": 2.0 ** -24, "float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}
+INF = float("inf")
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return torch
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _logits(torch, rows, vocab, dtype, seed, pad=0, sigma=3.0):
+    r = np.random.default_rng(seed)
+    z = r.normal(size=(rows, vocab)) * sigma
+    z += 8.0 * (r.random(z.shape) < 0.01)
+    full = torch.full((rows, vocab + pad), float("nan"), dtype=getattr(torch, dtype),
+                      device="cuda")
+    full[:, :vocab] = torch.from_numpy(z).to(full.dtype)
+    return full[:, :vocab]
+
+
+# ------------------------------------------------------------------ top logits
+
+def _top(torch, z, top, tau=1.0, **kw):
+    import paper_2202_06009_amd as zo
+    rows = z.shape[0]
+    values = torch.full((rows, top), 7.0, device="cuda")
+    columns = torch.full((rows, top), -7, dtype=torch.int32, device="cuda")
+    lse = torch.full((rows,), 7.0, device="cuda")
+    zo.zo_top_logits(z, values, columns, lse, tau=tau, **kw)
+    return values, columns, lse
+
+
+def _check_top(torch, z, top, tau=1.0, got=None):
+    values, columns, lse = got or _top(torch, z, top, tau)
+    z64 = _np(z)
+    wv, wc, wl = ref.top_logits(z64, top, tau)
+    np.testing.assert_array_equal(columns.cpu().numpy(), wc)
+    np.testing.assert_array_equal(_np(values), wv)
+    # |z| / tau rounded, exp and log to a few units, a sum of positive terms
+    finite = np.where(np.isfinite(z64), np.abs(z64), 0).max() / tau
+    tol = (4 * finite + np.log(z64.shape[1]) + 40) * 2.0 ** -23
+    same = _np(lse) == wl
+    np.testing.assert_array_equal(np.isnan(_np(lse)), np.isnan(wl))
+    with np.errstate(invalid="ignore"):
+        off = np.abs(_np(lse) - wl)
+    assert (same | np.isnan(wl) | (off <= tol)).all()
+
+
+TOPS = [(1, 1, 1), (3, 2, 2), (2, 7, 3), (1, 64, 64), (5, 255, 17), (4, 1000, 1), (3, 1023, 1000),
+        (2, 1024, 1024), (3, 1025, 1024), (7, 4097, 64), (2, 8191, 256), (1, 30522, 8),
+        (3, 50257, 8), (2, 50257, 300), (1, 131071, 5), (2, 200003, 64), (300, 999, 12)]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("shape", TOPS)
+def test_top_logits(torch, shape, dtype):
+    rows, vocab, top = shape
+    for pad, tau in ((0, 1.0), (3, 2.5)):
+        _check_top(torch, _logits(torch, rows, vocab, dtype, vocab + pad, pad), top, tau)
+
+
+@pytest.mark.parametrize("vocab", [130, 5000, 50257])
+@pytest.mark.parametrize("top", [1, 5, 64, 128])
+def test_top_ties_and_masks(torch, vocab, top):
+    """Constant rows, few distinct values, everything masked but fewer columns
+    than asked for, the type's lowest value, infinities, signed zeros, NaN; the
+    largest all in a run of neighbouring columns."""
+    r = np.random.default_rng(vocab + top)
+    z = torch.zeros((12, vocab), device="cuda")
+    z[1] = -INF
+    z[2] = torch.finfo(torch.float32).min
+    z[3] = torch.from_numpy(r.integers(0, 3, vocab)).float()
+    z[4] = -INF
+    z[4, vocab // 2:vocab // 2 + 3] = torch.tensor([1.0, 2.0, 1.0])
+    z[5] = torch.finfo(torch.float32).min
+    z[5, [3, vocab - 1]] = 0.5
+    z[6] = torch.where(torch.arange(vocab, device="cuda") % 2 == 0, 0.0, -0.0)
+    z[7].normal_()
+    z[7, 11], z[7, 12], z[7, 13] = INF, float("nan"), -float("nan")
+    z[8].normal_()
+    z[8, 100:130] = INF
+    z[9].normal_()
+    z[9, 1:129] += 1000.0
+    z[10] = -torch.arange(vocab, device="cuda").float()
+    z[11] = torch.arange(vocab, device="cuda").float()
+    for dtype in (torch.float32, torch.bfloat16):
+        _check_top(torch, z.to(dtype), top)
+
+
+def test_top_without_lse_on_a_stream_and_in_a_graph(torch):
+    import paper_2202_06009_amd as zo
+    for rows in (2, 70):
+        z = _logits(torch, rows, 20011, "bfloat16", 4)
+        values = torch.empty((rows, 9), device="cuda")
+        columns = torch.empty((rows, 9), dtype=torch.int32, device="cuda")
+        lse = torch.empty(rows, device="cuda")
+        zo.zo_top_logits(z, values, columns)
+        wv, wc, _ = ref.top_logits(_np(z), 9, 1.0)
+        np.testing.assert_array_equal(columns.cpu().numpy(), wc)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        values.zero_()
+        s.wait_stream(torch.cuda.current_stream())
+        zo.zo_top_logits(z, values, columns, lse, stream=s)
+        torch.cuda.current_stream().wait_stream(s)
+        _check_top(torch, z, 9, got=(values, columns, lse))
+        ws = torch.empty(zo.zo_top_logits_ws(rows, 20011, 9) or 1, dtype=torch.uint8,
+                         device="cuda")
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            zo.zo_top_logits(z, values, columns, lse, ws=ws)
+        for i in range(4):
+            z.normal_(std=2.0)
+            columns.zero_()
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            _check_top(torch, z, 9, got=(values, columns, lse))
+
+
+def test_top_offsets_beyond_32_bits(torch):
+    z = torch.zeros((33000, 66000), dtype=torch.bfloat16, device="cuda")
+    z[-40:].normal_()
+    values, columns, lse = _top(torch, z, 4)
+    _check_top(torch, z[-40:], 4, got=(values[-40:], columns[-40:], lse[-40:]))
+    assert (columns[0].cpu() == torch.arange(4)).all()
+
+
+# ---------------------------------------------------------------- distillation
+
+def _teacher(torch, z, top, tau, seed):
+    """A teacher near the student: its top logits, columns and log-sum-exp."""
+    r = np.random.default_rng(seed)
+    u = np.where(np.isfinite(_np(z)), _np(z), -INF) + r.normal(size=z.shape)
+    cols = np.argsort(-u, axis=1, kind="stable")[:, :top].astype(np.int32)
+    vals = np.take_along_axis(u, cols, 1).astype(np.float32)
+    lse = ref.log_sum_exp(u / tau).astype(np.float32)
+    return vals, cols, lse
+
+
+def _distill(torch, z, vals, cols, *, tau=1.0, lse=None, labels=None, kd=1.0, ce=0.0, weight=None,
+             inplace=False, pad=0, **kw):
+    import paper_2202_06009_amd as zo
+
+    def dev(a, dt):
+        return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).to(dt).cuda()
+    rows, vocab = z.shape
+    loss = torch.full((rows,), 7.0, device="cuda")
+    full = torch.full((rows, vocab + pad), 7.0, dtype=z.dtype, device="cuda")
+    dz = z if inplace else full[:, :vocab]
+    zo.zo_distill_loss(z, dev(vals, torch.float32), dev(cols, torch.int32), loss, dz, tau=tau,
+                       teacher_lse=dev(lse, torch.float32), labels=dev(labels, torch.int32),
+                       kd_weight=kd, ce_weight=ce, row_weight=dev(weight, torch.float32), **kw)
+    if not inplace:
+        assert (full[:, vocab:] == 7.0).all()
+    return loss, dz
+
+
+def _check_distill(torch, z, vals, cols, *, tau=1.0, lse=None, labels=None, kd=1.0, ce=0.0,
+                   weight=None, **kw):
+    z64 = _np(z)
+    got_loss, got_dz = _distill(torch, z, vals, cols, tau=tau, lse=lse, labels=labels, kd=kd,
+                                ce=ce, weight=weight, **kw)
+    want_loss, want_dz = ref.distill(z64, vals.astype(np.float64), cols, tau=tau, lse=lse,
+                                     labels=labels, kd=kd, ce=ce, weight=weight)
+    got_loss, got_dz = _np(got_loss), _np(got_dz)
+    # every probability is exp of a difference of numbers up to `big`, each rounded once
+    # or twice in binary32, so it is off by eps of itself; so are sums of them
+    def top_of(a):
+        a = np.abs(a[np.isfinite(a)])
+        return a.max() if a.size else 0.0
+    fine = (np.asarray(weight) != 0) if weight is not None else np.ones(len(z64), bool)
+    big = (top_of(z64[fine]) + top_of(vals) + (top_of(lse) if lse is not None else 0))
+    eps = (4 * big * max(1.0, 1 / tau) + 64) * 2.0 ** -23
+    w = np.abs(np.asarray(weight, np.float64)) if weight is not None else np.ones(len(z64))
+    size = kd * tau * tau + ce
+    same = (got_loss == want_loss) | (np.isnan(got_loss) & np.isnan(want_loss))
+    with np.errstate(invalid="ignore"):
+        off = np.abs(got_loss - want_loss)
+    # the log of a probability is off by eps, times probabilities that sum to at most 1;
+    # what the teacher leaves of 1 is off by eps, times a log of at most ~100
+    lim = w * size * eps * (110 if lse is not None else 3)
+    assert (same | (off <= lim)).all(), (got_loss, want_loss, lim)
+    # gradient: a few probabilities of at most 1, each off by eps of itself; the part that
+    # the teacher leaves is off by eps as a whole, spread as the student spreads it
+    name = str(z.dtype).replace("torch.", "")
+    unit = w[:, None] * (kd * tau + ce)
+    with np.errstate(over="ignore"):
+        off = np.abs(got_dz - want_dz)
+    # q and p themselves bound each term
+    s = z64 / tau
+    q = np.zeros(z64.shape)
+    for t in range(len(z64)):
+        if fine[t]:
+            tot = ref.log_sum_exp(s[t][None])[0]
+            one = ref.log_sum_exp(z64[t][None])[0]
+            if np.isfinite(tot):
+                q[t] = np.exp(s[t] - tot) + np.exp(z64[t] - one)
+                if lse is not None:
+                    ins = np.zeros(z64.shape[1], bool)
+                    ins[[c for c in cols[t] if 0 <= c < z64.shape[1]]] = True
+                    rest = ref.log_sum_exp(s[t][None, ~ins])[0] if (~ins).any() else -INF
+                    if rest != -INF:
+                        q[t, ~ins] += np.exp(s[t, ~ins] - rest)
+            for j, c in enumerate(cols[t]):
+                if 0 <= c < z64.shape[1]:
+                    q[t, c] += 1.0
+            if labels is not None and 0 <= labels[t] < z64.shape[1]:
+                q[t, labels[t]] += 1.0
+    lim = unit * q * eps + HALF_ULP[name] * (np.abs(want_dz) + unit * q * eps)
+    lim = lim + (2.0 ** -25 if name == "float16" else 2.0 ** -120)
+    bad = ~((off <= lim) | (np.isnan(got_dz) & np.isnan(want_dz)))
+    assert not bad.any(), (np.argwhere(bad)[:5], got_dz[bad][:5], want_dz[bad][:5], lim[bad][:5])
+
+
+DISTILLS = [(1, 1, 1), (2, 2, 1), (3, 7, 7), (2, 8, 3), (1, 64, 64), (3, 129, 5), (2, 1000, 1000),
+            (4, 1025, 32), (2, 8191, 100), (2, 30522, 16), (1, 50257, 64), (2, 70001, 200),
+            (1, 131072, 8), (1, 262144, 1024), (70, 515, 9)]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("shape", DISTILLS)
+def test_distill(torch, shape, dtype):
+    rows, vocab, top = shape
+    r = np.random.default_rng(vocab)
+    for pad, tau, tail, ce in ((0, 1.0, False, 0.0), (3, 2.0, True, 0.0), (8, 1.5, True, 0.3),
+                               (1, 4.0, False, 0.5)):
+        z = _logits(torch, rows, vocab, dtype, vocab + pad, pad)
+        vals, cols, lse = _teacher(torch, z, top, tau, pad)
+        if rows > 1:                                 # some slots unused
+            cols[1, top // 2:] = -1
+        labels = r.integers(-1, vocab, rows).astype(np.int32) if ce else None
+        if ce:
+            labels[0] = cols[0, 0]
+        weight = r.normal(size=rows).astype(np.float32) if pad else None
+        _check_distill(torch, z, vals, cols, tau=tau, lse=lse if tail else None, labels=labels,
+                       kd=0.7, ce=ce, weight=weight, pad=pad)
+
+
+@pytest.mark.parametrize("vocab", [40, 3001, 50257])
+@pytest.mark.parametrize("tail", [False, True])
+def test_distill_masks(torch, vocab, tail):
+    """Rows with no used slot, repeated and out-of-range columns, a masked student
+    and teacher (-infinity and the type's lowest value), a row that leaves the student
+    nothing, rows of weight 0 that hold NaN."""
+    rows, top = 9, 6
+    z = _logits(torch, rows, vocab, "float32", 1)
+    vals, cols, lse = _teacher(torch, z, top, 1.0, 2)
+    cols[0] = [-1, vocab, 2 ** 31 - 1, -2 ** 31, -5, vocab + 7]      # nothing used
+    cols[1] = [5, 5, 9, 5, 9, 11]                                    # repeats: the first counts
+    vals[1] -= 6.0
+    vals[2, 3:] = -INF                                               # a masked teacher
+    z[3, cols[3, 0]] = -INF                                          # excluded by the student
+    mask = np.ones(vocab, bool)
+    mask[cols[4]] = False
+    z[4, torch.from_numpy(mask)] = -INF                              # student: only S is left
+    lse[4] = ref.log_sum_exp(vals[4][None].astype(np.float64))[0] - 1e-3
+    z[5, ::2] = torch.finfo(torch.float32).min
+    vals[5] = np.where(np.isin(cols[5] % 2, [1]), vals[5], -1e30)
+    z[6] = -INF                                                      # nothing is left
+    z[7] = float("nan")
+    weight = np.ones(rows, np.float32)
+    weight[7] = 0.0                                                  # not read
+    weight[8] = -2.5
+    labels = np.array([3, -1, vocab, 7, -1, 1, -1, 0, 2], np.int32)
+    for ce in (0.0, 0.5):
+        _check_distill(torch, z, vals, cols, lse=lse if tail else None, labels=labels, ce=ce,
+                       weight=weight)
+
+
+@pytest.mark.parametrize("tail", [False, True])
+def test_distill_excluded_labels(torch, tail):
+    """A label whose logit is -infinity, and a row that is all -infinity with one."""
+    z = _logits(torch, 3, 600, "float32", 8)
+    vals, cols, lse = _teacher(torch, z, 4, 1.0, 2)
+    labels = np.array([77, 5, 9], np.int32)
+    z[0, 77] = -INF
+    z[1] = -INF
+    _check_distill(torch, z, vals, cols, lse=lse if tail else None, labels=labels, ce=0.5)
+    _check_distill(torch, z, vals, cols, lse=lse if tail else None, labels=labels, kd=0.0, ce=1.0)
+
+
+def test_distill_in_place_and_parts(torch):
+    """The gradient over the logits themselves; the loss or the gradient alone."""
+    import paper_2202_06009_amd as zo
+    for rows, vocab, dtype in ((3, 1003, "float32"), (2, 50257, "bfloat16"), (600, 777, "float16")):
+        z = _logits(torch, rows, vocab, dtype, 9, pad=5)
+        vals, cols, lse = _teacher(torch, z, 20, 1.0, 3)
+        loss, dz = _distill(torch, z, vals, cols, lse=lse)
+        v, c, l = (torch.from_numpy(a).cuda() for a in (vals, cols, lse))
+        alone = torch.empty(rows, device="cuda")
+        zo.zo_distill_loss(z, v, c, alone, teacher_lse=l)
+        assert torch.equal(alone, loss)
+        grad = torch.empty_like(dz)
+        zo.zo_distill_loss(z, v, c, None, grad, teacher_lse=l)
+        assert torch.equal(grad, dz)
+        loss2, dz2 = _distill(torch, z, vals, cols, lse=lse, inplace=True)
+        assert torch.equal(loss2, loss) and torch.equal(dz2, dz)
+
+
+def test_distill_gradient_is_the_difference_quotient(torch):
+    """The kernel's gradient against differences of the kernel's own loss.  A step h
+    along a direction d changes the loss by h <dz, d> up to h^3 / 6 times a third
+    derivative of at most sum |d|^3 and the rounding of two losses."""
+    rows, vocab, top, tau = 40, 301, 12, 1.3
+    z = _logits(torch, rows, vocab, "float32", 21, sigma=1.0)
+    vals, cols, lse = _teacher(torch, z, top, tau, 22)
+    labels = np.arange(rows, dtype=np.int32) * 3
+    for kw in (dict(), dict(lse=lse), dict(lse=lse, labels=labels, ce=0.5)):
+        kw = dict(kw, tau=tau)
+        _, dz = _distill(torch, z, vals, cols, **kw)
+        d = torch.zeros_like(z)
+        d.normal_(generator=torch.Generator(device="cuda").manual_seed(5))
+        d /= d.norm(dim=1, keepdim=True)
+        h = 2.0 ** -5
+        up = _np(_distill(torch, z + h * d, vals, cols, **kw)[0])
+        dn = _np(_distill(torch, z - h * d, vals, cols, **kw)[0])
+        slope = (up - dn) / (2 * h)
+        want = (_np(dz) * _np(d)).sum(1)
+        # third derivative: cumulants of a direction of length 1, at most 2 per softmax
+        assert np.abs(slope - want).max() <= h * h / 6 * 2 * (tau * tau + 1.0) + 60 * 2.0 ** -21 / h
+
+
+def test_distill_offsets_beyond_32_bits(torch):
+    z = torch.zeros((33000, 66000), dtype=torch.bfloat16, device="cuda")
+    z[-3:].normal_()
+    vals, cols, lse = _teacher(torch, z[-3:], 5, 1.0, 3)
+    v = torch.zeros((33000, 5), device="cuda")
+    c = torch.full((33000, 5), -1, dtype=torch.int32, device="cuda")
+    v[-3:], c[-3:] = torch.from_numpy(vals).cuda(), torch.from_numpy(cols).cuda()
+    import paper_2202_06009_amd as zo
+    loss = torch.full((33000,), 7.0, device="cuda")
+    dz = torch.full_like(z, 7.0)
+    zo.zo_distill_loss(z, v, c, loss, dz)
+    wl, wd = ref.distill(_np(z[-3:]), vals.astype(np.float64), cols)
+    assert not loss[:-3].any() and not dz[:1000].any() and not dz[-4].any()
+    assert np.abs(_np(loss[-3:]) - wl).max() <= 200 * 2.0 ** -23
+    assert np.abs(_np(dz[-3:]) - wd).max() <= 2.0 ** -8
+
+
+def test_distill_on_a_stream_and_in_a_graph(torch):
+    import paper_2202_06009_amd as zo
+    for rows in (2, 90):
+        z = _logits(torch, rows, 9001, "float32", 2)
+        vals, cols, lse = _teacher(torch, z, 7, 1.0, 3)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        v, c, l = (torch.from_numpy(a).cuda() for a in (vals, cols, lse))
+        loss, dz = torch.zeros(rows, device="cuda"), torch.zeros_like(z)
+        s.wait_stream(torch.cuda.current_stream())
+        zo.zo_distill_loss(z, v, c, loss, dz, teacher_lse=l, stream=s)
+        torch.cuda.current_stream().wait_stream(s)
+        again, dz2 = _distill(torch, z, vals, cols, lse=lse)
+        assert torch.equal(loss, again) and torch.equal(dz, dz2)
+        ws = torch.empty(zo.zo_distill_ws(rows, 9001) or 1, dtype=torch.uint8, device="cuda")
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            zo.zo_distill_loss(z, v, c, loss, dz, teacher_lse=l, ws=ws)
+        for i in range(4):
+            z.normal_()
+            loss.zero_()
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            again, dz2 = _distill(torch, z, vals, cols, lse=lse)
+            assert torch.equal(loss, again) and torch.equal(dz, dz2)
+
+
+def test_logit_wrappers_refuse(torch):
+    import paper_2202_06009_amd as zo
+    z = torch.zeros((2, 50), device="cuda")
+    v, c = torch.zeros((2, 3), device="cuda"), torch.zeros((2, 3), dtype=torch.int32, device="cuda")
+    loss = torch.zeros(2, device="cuda")
+    with pytest.raises(ValueError):
+        zo.zo_top_logits(z, v, c.long())
+    with pytest.raises(ValueError):
+        zo.zo_top_logits(z, v[:1], c)
+    with pytest.raises(ValueError):
+        zo.zo_top_logits(z.t(), v, c)
+    with pytest.raises(zo.ZoError):
+        zo.zo_top_logits(z, v, c, tau=0.0)
+    with pytest.raises(zo.ZoError):
+        zo.zo_distill_loss(z, v, c)
+    with pytest.raises(ValueError):
+        zo.zo_distill_loss(z, v, c, loss, z.bfloat16())
+    with pytest.raises(ValueError):
+        zo.zo_distill_loss(z, v, c, loss, labels=torch.zeros(2, dtype=torch.int64, device="cuda"))
+    with pytest.raises(ValueError):
+        zo.zo_distill_loss(z, v, c, loss.double())
