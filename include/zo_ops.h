@@ -172,9 +172,10 @@ int64_t zo_distill_ws(int64_t rows, int64_t vocab);
  *     d = q - p on S; outside S d = q, with L q - p_r (q / q_r).
  * A part whose weight is 0 is left out.  Outcomes with p = 0 add 0 to KL; one with p > 0 that the student excludes
  * (logits of -infinity) makes the loss +infinity and leaves the gradient
- * finite, and so does an excluded label.  p_r below 2^-16 counts as 0 where the student excludes everything
- * outside S: it is no more than the rounding of L.  A student row of only
- * -infinity has q = 0.  No used slot: no KL part without L; with L, p_r = q_r = 1.
+ * finite, and so does an excluded label.  p_r below 2^-16 counts as 0 where
+ * the student excludes everything outside S: it is no more than the rounding
+ * of L.  A student row of only -infinity has q = 0.  Without L, a row whose used
+ * slots hold no teacher's logit above -infinity has no KL part.
  */
 int zo_distill_loss(const zo_distill *args, hipStream_t stream);
 

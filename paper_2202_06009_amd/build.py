@@ -17,7 +17,7 @@ SOURCES = [os.path.join(CSRC, f) for f in ("zo_kernels.hip", "zo_server.hip",
                                            "zo_server_many.hip", "zo_server_ua.hip",
                                            "zo_kernels_ua.hip", "zo_adam.cpp",
                                            "zo_mx4_quant.hip", "zo_mx4_gemm.hip",
-                                           "zo_logits.hip", "zo_ops.cpp")]
+                                           "zo_top.hip", "zo_distill.hip", "zo_ops.cpp")]
 HEADERS = [os.path.join(ROOT, "include", "zo_adam.h"), os.path.join(ROOT, "include", "zo_ops.h"),
            os.path.join(CSRC, "zo_internal.h"), os.path.join(CSRC, "zo_ops_internal.h"),
            os.path.join(CSRC, "zo_ops_device.h"),

@@ -1,0 +1,569 @@
+// zo_distill.hip -- the distillation loss from a teacher's top logits and the
+// gradient of the student's logits.
+//
+// One workgroup per row, one pass over memory: the row stays in registers
+// (k_distill) between the statistics and the gradient, so that a row costs one
+// read and one write.  S (the columns of the used slots) is marked by a bit per
+// column in shared memory; its logits are taken out of the row (as -infinity)
+// and belong to the threads that hold the slots.  All sums over the rest, of
+//   e_i = 2^(c z_i - b), c = log2(e) / tau, b = the rest's own largest c z, rounded,
+// are then the rest's own, with no 1 - sum: q_i / q_r = e_i / sum e keeps its
+// digits however little the rest holds.  The gradient of the rest is e_i times
+// one factor of the row, and at tau = 1 and tau = 2 the label's softmax follows
+// from the same e_i (e_i, e_i^2): one exponential per logit in each of the two
+// sweeps instead of two.
+//
+// c z - b is one fused operation, rounded relative to itself; b's own rounding
+// is common to every term and cancels.  Where c z could overflow (the row's
+// largest logit is near the end of binary32) and in rows that do not fit
+// registers (k_distill_long, two reads), the difference z - b is formed first,
+// b being the largest logit itself (FAR).
+#include "zo_ops_device.h"
+
+namespace zo {
+
+constexpr int kMaxTop = 1024;
+
+// What 1 - sum p is known to, its terms being rounded exponentials of numbers
+// around 10: where the student has nothing outside S, less than this is nothing.
+constexpr float kRestRounding = 0x1p-16f;
+
+// The base b of a sum whose largest logit is m; 0 for an empty sum.
+template <bool FAR>
+__device__ __forceinline__ float base_of(float m, float c)
+{
+    return m == -INFINITY ? 0.0f : FAR ? m : m * c;
+}
+
+// log2 of e for logit z.
+template <bool FAR>
+__device__ __forceinline__ float above(float z, float c, float b)
+{
+    return FAR ? (z - b) * c : __builtin_fmaf(z, c, -b);
+}
+
+// log2 of the factor from base b to base to.
+template <bool FAR>
+__device__ __forceinline__ float between(float b, float to, float c)
+{
+    return FAR ? (b - to) * c : b - to;
+}
+
+// How the label's softmax (tau = 1) follows from e: not wanted; e; e^2; by an
+// exponential of its own.
+enum LabelForm { kNoLabel, kSame, kSquare, kOwn };
+
+// A slot of the teacher: its column (-1: unused), the two logits, and, once the
+// row's statistics are known, the two probabilities.
+struct Slot {
+    int32_t col;
+    float u, z, p, q;
+};
+
+template <int TH>
+struct DistillShared {
+    int32_t col[kMaxTop];
+    float red[12][TH / 64];
+    int dup;
+};
+
+template <int TH>
+struct Row {
+    static constexpr int NS = kMaxTop / TH, NW = TH / 64;
+    int64_t row, V;
+    float w, c;              // weight, log2(e) / tau
+    int32_t y;               // label, or -1
+    float zy;
+    bool tail;
+    LabelForm form;
+    Slot slot[NS];
+};
+
+// What a row's gradient follows from, besides its logits.
+struct Stats {
+    float b_out, b_all, b_one;          // bases: outside S, all, all at tau = 1
+    float s_out, s_all, s_one;          // and sums
+    float share;                        // q_i = share e_i outside S
+    float pr;                           // teacher's mass outside S
+    float gk, ge;                       // factors of the two parts
+    bool kd, none, no_rest;
+};
+
+__device__ __forceinline__ bool is_marked(const uint32_t *bits, int64_t i)
+{
+    return bits[i >> 5] >> (i & 31) & 1;
+}
+
+// The marks of the kVec columns from column i (a multiple of kVec) on.
+template <int GT>
+__device__ __forceinline__ uint32_t marks_of(const uint32_t *bits, int64_t i)
+{
+    const uint32_t byte = reinterpret_cast<const uint8_t *>(bits)[i >> 3];
+    return GT == GT_F32 ? byte >> (i & 4) & 15u : byte;
+}
+
+// The row's scalars; its slots, S marked.  Synchronises; false: weight 0.
+template <int GT, int TH>
+__device__ __forceinline__ bool read_row(const zo_distill &a, Row<TH> &R, DistillShared<TH> &s,
+                                         uint32_t *bits, const typename Elem<GT>::T *z)
+{
+    const int tid = threadIdx.x;
+    R.row = blockIdx.x;
+    R.V = a.vocab;
+    R.c = kLog2e / a.tau;
+    R.tail = a.teacher_lse != nullptr;
+    R.w = a.row_weight ? a.row_weight[R.row] : 1.0f;
+    if (R.w == 0.0f) return false;
+    R.y = a.labels && a.ce_weight != 0.0f ? a.labels[R.row] : -1;
+    if (R.y < 0 || R.y >= R.V) R.y = -1;
+    R.zy = R.y >= 0 ? widen<GT>(z[R.y]) : 0.0f;
+    R.form = R.y < 0 ? kNoLabel : a.tau == 1.0f ? kSame : a.tau == 2.0f ? kSquare : kOwn;
+    for (int i = tid; i < (int)((R.V + 31) / 32); i += TH) bits[i] = 0;
+    if (tid == 0) s.dup = 0;
+#pragma unroll
+    for (int n = 0; n < R.NS; ++n) {
+        const int j = n * TH + tid;
+        Slot t = {-1, -INFINITY, -INFINITY, 0.0f, 0.0f};
+        if (j < a.top) {
+            const int32_t col = a.columns[R.row * a.top + j];
+            if (col >= 0 && col < R.V)
+                t = {col, a.values[R.row * a.top + j], widen<GT>(z[col]), 0.0f, 0.0f};
+            s.col[j] = t.col;
+        }
+        R.slot[n] = t;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < R.NS; ++n) {
+        const int32_t col = R.slot[n].col;
+        if (col >= 0 && (atomicOr(&bits[col >> 5], 1u << (col & 31)) >> (col & 31) & 1))
+            s.dup = 1;
+    }
+    __syncthreads();
+    if (s.dup) {                        // of equal columns the first counts
+#pragma unroll
+        for (int n = 0; n < R.NS; ++n) {
+            bool again = false;
+            if (R.slot[n].col >= 0)
+                for (int i = 0; i < n * TH + tid; ++i) again |= s.col[i] == R.slot[n].col;
+            if (again) R.slot[n] = {-1, -INFINITY, -INFINITY, 0.0f, 0.0f};
+        }
+    }
+    return true;
+}
+
+// Joins the threads' sums outside S (s_out about b_out; at tau = 1: s1 about b1,
+// unless it follows from e) with the slots; writes the loss.  m_in: the slots'
+// largest logit, um the largest teacher's.  Synchronises.
+template <bool FAR, int TH>
+__device__ __forceinline__ Stats statistics(const zo_distill &a, Row<TH> &R,
+                                            DistillShared<TH> &s, float m_out, float m_in,
+                                            float um, float s_out, float s1)
+{
+    constexpr int NW = Row<TH>::NW;
+    Stats t;
+    const float m_all = fmaxf(m_out, m_in), c = R.c;
+    t.b_out = base_of<FAR>(m_out, c);
+    t.b_all = base_of<FAR>(m_all, c);
+    t.b_one = base_of<FAR>(m_all, kLog2e);
+    t.gk = R.w * a.kd_weight * a.tau;
+    t.ge = R.w * a.ce_weight;
+    t.kd = a.kd_weight != 0.0f && (R.tail || um != -INFINITY);
+    const float lse = R.tail ? a.teacher_lse[R.row] : 0.0f, u0 = R.tail ? 0.0f : um;
+    float logp[Row<TH>::NS], s_in = 0.0f, one_in = 0.0f, psum = 0.0f;
+#pragma unroll
+    for (int n = 0; n < R.NS; ++n) {
+        const Slot &k = R.slot[n];
+        logp[n] = -INFINITY;
+        if (k.col < 0) continue;
+        if (k.u != -INFINITY) logp[n] = (k.u - u0) / a.tau - lse;
+        psum += expf(logp[n]);
+        s_in += exp2_hw(above<FAR>(k.z, c, t.b_all));
+        if (R.form == kSquare)
+            one_in += exp2_hw(2.0f * above<FAR>(k.z, c, t.b_all));
+        else if (R.form == kOwn)
+            one_in += exp2_hw(above<FAR>(k.z, kLog2e, t.b_one));
+    }
+    group_put<OpSum>(s_out, s.red[4]);
+    group_put<OpSum>(s1, s.red[5]);
+    group_put<OpSum>(s_in, s.red[6]);
+    group_put<OpSum>(one_in, s.red[7]);
+    group_put<OpSum>(psum, s.red[8]);
+    __syncthreads();
+    t.s_out = group_get<OpSum, NW>(s.red[4]);
+    s1 = group_get<OpSum, NW>(s.red[5]);
+    s_in = group_get<OpSum, NW>(s.red[6]);
+    one_in = group_get<OpSum, NW>(s.red[7]);
+    psum = group_get<OpSum, NW>(s.red[8]);
+    t.no_rest = m_out == -INFINITY && t.s_out == 0.0f;
+    t.none = t.no_rest && m_in == -INFINITY && s_in == 0.0f;
+    const float log_to_all = m_out == -INFINITY ? 0.0f : between<FAR>(t.b_out, t.b_all, c);
+    const float to_all = exp2_hw(log_to_all);
+    t.s_all = t.s_out * to_all + s_in;
+    t.share = t.none ? 0.0f : to_all / t.s_all;
+    if (R.form == kSame)
+        t.s_one = t.s_all;
+    else if (R.form == kSquare)
+        t.s_one = s1 * exp2_hw(2.0f * log_to_all) + one_in;
+    else
+        t.s_one = s1 + one_in;
+    if (R.form == kSame || R.form == kSquare) t.b_one = t.b_all;
+    t.pr = 0.0f;
+    if (R.tail) {
+        t.pr = fmaxf(0.0f, 1.0f - psum);
+        if (t.no_rest && t.pr < kRestRounding) t.pr = 0.0f;
+    }
+    const float log_p = R.tail ? 0.0f : logf(psum), log_all = logf(t.s_all);
+    // p log(p / q) - p + q for each outcome: what is added sums to 0 over all
+    // outcomes, and a term is then small where p is near q
+    float kl = 0.0f, qsum = 0.0f;
+#pragma unroll
+    for (int n = 0; n < R.NS; ++n) {
+        Slot &k = R.slot[n];
+        if (k.col < 0) continue;
+        const float l = above<FAR>(k.z, c, t.b_all);
+        k.p = expf(logp[n] - log_p);
+        k.q = t.none ? 0.0f : exp2_hw(l) / t.s_all;
+        if (k.p == 0.0f)
+            kl += k.q;
+        else if (t.none || k.z == -INFINITY)
+            kl = INFINITY;
+        else
+            kl += k.p * ((logp[n] - log_p) - (l * kLn2 - log_all)) - k.p + k.q;
+        qsum += k.q;
+    }
+    if (!a.loss) return t;
+    group_put<OpSum>(kl, s.red[9]);
+    group_put<OpSum>(qsum, s.red[10]);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        kl = group_get<OpSum, NW>(s.red[9]);
+        qsum = group_get<OpSum, NW>(s.red[10]);
+        if (R.tail) {
+            const float qr = t.s_out * t.share;
+            kl += t.pr > 0.0f ? (qr > 0.0f ? t.pr * logf(t.pr / qr) - t.pr + qr : INFINITY) : qr;
+            kl += fmaxf(0.0f, psum - 1.0f);
+        } else if (!t.none) {
+            kl += 1.0f - qsum;
+        }
+        float l = 0.0f;
+        if (t.kd) l = a.kd_weight * a.tau * a.tau * kl;
+        if (R.y >= 0) {
+            const float lz = R.form == kOwn ? above<FAR>(R.zy, kLog2e, t.b_one)
+                                            : above<FAR>(R.zy, c, t.b_one) * a.tau;
+            l += a.ce_weight * (R.zy == -INFINITY ? INFINITY : logf(t.s_one) - lz * kLn2);
+        }
+        a.loss[R.row] = R.w * l;
+    }
+    return t;
+}
+
+// The gradient outside S of kVec logits from column i on, as e times the row's
+// factors; f_out: gradient per e, f_one: the label's softmax per its exponential.
+template <int GT, bool FAR, LabelForm FORM>
+__device__ __forceinline__ u32x4 rest_gradient(const u32x4 &w, int64_t i, float c, const Stats &t,
+                                               float f_out, float f_one, int32_t y)
+{
+    constexpr int K = Elem<GT>::kVec;
+    float d[K];
+#pragma unroll
+    for (int q = 0; q < K; ++q) {
+        const float z = elem_of<GT>(w, q);
+        const float e = exp2_hw(above<FAR>(z, c, t.b_out));
+        if constexpr (FORM == kNoLabel || FORM == kSame)
+            d[q] = f_out * e;
+        else if constexpr (FORM == kSquare)
+            d[q] = e * __builtin_fmaf(f_one, e, f_out);
+        else
+            d[q] = __builtin_fmaf(f_out, e, f_one * exp2_hw(above<FAR>(z, kLog2e, t.b_one)));
+    }
+    if constexpr (FORM != kNoLabel) {
+        const uint32_t at = (uint32_t)(y - (int32_t)i);
+        if (at < (uint32_t)K) {
+#pragma unroll
+            for (int q = 0; q < K; ++q)
+                if (at == (uint32_t)q) d[q] -= t.ge;
+        }
+    }
+    return pack16<GT>(d);
+}
+
+// Stores kVec gradients of which those in S are another thread's.
+template <int GT>
+__device__ __forceinline__ void store_rest(typename Elem<GT>::T *dz, int64_t i, int64_t V,
+                                           const u32x4 &d, uint32_t marks)
+{
+    using T = typename Elem<GT>::T;
+    if (marks == 0) {
+        store16<GT>(dz + i, d, V - i);
+        return;
+    }
+#pragma unroll
+    for (int q = 0; q < Elem<GT>::kVec; ++q)
+        if (i + q < V && !(marks >> q & 1))
+            dz[i + q] = GT == GT_F32 ? (T)d[q & 3] : (T)(d[(q >> 1) & 3] >> (16 * (q & 1)));
+}
+
+// Factors of rest_gradient.
+template <bool FAR>
+__device__ __forceinline__ void rest_factors(const Stats &t, LabelForm form, float c, float &f_out,
+                                             float &f_one)
+{
+    f_out = !t.kd || t.no_rest ? 0.0f : t.gk * (t.share - t.pr / t.s_out);
+    f_one = 0.0f;
+    if (form == kNoLabel || t.no_rest) return;
+    if (form == kSame) {
+        f_out += t.ge * t.share;
+    } else {
+        const float shift = form == kSquare ? 2.0f * between<FAR>(t.b_out, t.b_all, c) : 0.0f;
+        f_one = t.ge * exp2_hw(shift) / t.s_one;
+    }
+}
+
+// The gradient at the thread's slots.
+template <int GT, bool FAR, int TH>
+__device__ __forceinline__ void slot_gradient(const Row<TH> &R, const Stats &t, float tau,
+                                              typename Elem<GT>::T *dz)
+{
+#pragma unroll
+    for (int n = 0; n < R.NS; ++n) {
+        const Slot &k = R.slot[n];
+        if (k.col < 0) continue;
+        float d = t.kd ? t.gk * (k.q - k.p) : 0.0f;
+        if (R.form != kNoLabel) {
+            const float l = R.form == kOwn ? above<FAR>(k.z, kLog2e, t.b_one)
+                                           : above<FAR>(k.z, R.c, t.b_one) * tau;
+            d += t.ge * ((t.none ? 0.0f : exp2_hw(l) / t.s_one) - (k.col == R.y ? 1.0f : 0.0f));
+        }
+        dz[k.col] = narrow<GT>(d);
+    }
+}
+
+// Calls f(integral_constant<FORM>).
+template <class F>
+__device__ __forceinline__ void with_form(LabelForm form, F &&f)
+{
+    switch (form) {
+    case kNoLabel: f(std::integral_constant<LabelForm, kNoLabel>{}); break;
+    case kSame: f(std::integral_constant<LabelForm, kSame>{}); break;
+    case kSquare: f(std::integral_constant<LabelForm, kSquare>{}); break;
+    case kOwn: f(std::integral_constant<LabelForm, kOwn>{}); break;
+    }
+}
+
+// The slots' largest logits.
+template <int TH>
+__device__ __forceinline__ void slot_maxima(const Row<TH> &R, float &m_in, float &um)
+{
+    m_in = um = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < R.NS; ++n) {
+        m_in = fmaxf(m_in, R.slot[n].z);
+        um = fmaxf(um, R.slot[n].u);
+    }
+}
+
+template <int GT, int TH>
+__device__ __forceinline__ void skip_row(const zo_distill &a, int64_t row,
+                                         typename Elem<GT>::T *dz)
+{
+    constexpr int K = Elem<GT>::kVec;
+    if (a.loss && threadIdx.x == 0) a.loss[row] = 0.0f;
+    if (dz)
+        for (int64_t i = (int64_t)threadIdx.x * K; i < a.vocab; i += TH * K)
+            store16<GT>(dz + i, u32x4{0, 0, 0, 0}, a.vocab - i);
+}
+
+// Sums and gradient of a row in registers.
+template <int GT, int TH, int NV, bool FAR>
+__device__ __forceinline__ void resident_row(const zo_distill &a, Row<TH> &R,
+                                             DistillShared<TH> &s, const uint32_t *bits,
+                                             const u32x4 (&w)[NV], float m_out, float m_in,
+                                             float um, typename Elem<GT>::T *dz)
+{
+    constexpr int K = Elem<GT>::kVec;
+    const float c = R.c, b = base_of<FAR>(m_out, c);
+    const float b1 = base_of<FAR>(fmaxf(m_out, m_in), kLog2e);
+    float sum = 0.0f, one = 0.0f;
+    with_form(R.form, [&](auto form) {
+        constexpr LabelForm F = decltype(form)::value;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int q = 0; q < K; ++q) {
+                const float z = elem_of<GT>(w[v], q), e = exp2_hw(above<FAR>(z, c, b));
+                sum += e;
+                if constexpr (F == kSquare) one = __builtin_fmaf(e, e, one);
+                if constexpr (F == kOwn) one += exp2_hw(above<FAR>(z, kLog2e, b1));
+            }
+    });
+    const Stats t = statistics<FAR>(a, R, s, m_out, m_in, um, sum, one);
+    if (!dz) return;
+    float f_out, f_one;
+    rest_factors<FAR>(t, R.form, c, f_out, f_one);
+    with_form(R.form, [&](auto form) {
+        constexpr LabelForm F = decltype(form)::value;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int64_t i = (int64_t)(v * TH + (int)threadIdx.x) * K;
+            if (i >= R.V) break;
+            store_rest<GT>(dz, i, R.V,
+                           rest_gradient<GT, FAR, F>(w[v], i, c, t, f_out, f_one, R.y),
+                           marks_of<GT>(bits, i));
+        }
+    });
+    slot_gradient<GT, FAR>(R, t, a.tau, dz);
+}
+
+template <int GT, int TH, int NV>
+__global__ __launch_bounds__(TH) void k_distill(zo_distill a)
+{
+    using T = typename Elem<GT>::T;
+    constexpr int K = Elem<GT>::kVec, NW = TH / 64;
+    extern __shared__ uint32_t bits[];
+    __shared__ DistillShared<TH> s;
+    const T *z = static_cast<const T *>(a.z) + (int64_t)blockIdx.x * a.ldz;
+    T *dz = a.dz ? static_cast<T *>(a.dz) + (int64_t)blockIdx.x * a.lddz : nullptr;
+    Row<TH> R;
+    if (a.row_weight && a.row_weight[blockIdx.x] == 0.0f) {
+        skip_row<GT, TH>(a, blockIdx.x, dz);
+        return;
+    }
+    u32x4 w[NV];
+    load_row<GT, TH, NV>(w, z, a.vocab);      // in flight while the slots are read
+    read_row<GT, TH>(a, R, s, bits, z);
+    float m_out = -INFINITY, m_in, um;
+    slot_maxima(R, m_in, um);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int64_t i = (int64_t)(v * TH + (int)threadIdx.x) * K;
+        const uint32_t marks = i < R.V ? marks_of<GT>(bits, i) : 0u;
+        if (marks) {
+#pragma unroll
+            for (int q = 0; q < K; ++q)
+                if (marks >> q & 1) {
+                    if constexpr (GT == GT_F32)
+                        w[v][q] = kNegInf<GT>;
+                    else
+                        w[v][q >> 1] = q & 1 ? (w[v][q >> 1] & 0xFFFFu) | kNegInf<GT> << 16
+                                             : (w[v][q >> 1] & 0xFFFF0000u) | kNegInf<GT>;
+                }
+        }
+        m_out = fmaxf(m_out, max_of<GT>(w[v]));
+    }
+    group_put<OpMax>(m_out, s.red[0]);
+    group_put<OpMax>(m_in, s.red[1]);
+    group_put<OpMax>(um, s.red[2]);
+    __syncthreads();
+    m_out = group_get<OpMax, NW>(s.red[0]);
+    m_in = group_get<OpMax, NW>(s.red[1]);
+    um = group_get<OpMax, NW>(s.red[2]);
+    // -infinity has base 0; of the others the products with both factors must be finite
+    const float lo = fminf(m_out == -INFINITY ? 0.0f : m_out, m_in == -INFINITY ? 0.0f : m_in);
+    const float size = fmaxf(fabsf(lo), fmaxf(fabsf(fmaxf(m_out, 0.0f)), fmaxf(m_in, 0.0f)));
+    if (size * fmaxf(R.c, kLog2e) < 0x1p126f)
+        resident_row<GT, TH, NV, false>(a, R, s, bits, w, m_out, m_in, um, dz);
+    else
+        resident_row<GT, TH, NV, true>(a, R, s, bits, w, m_out, m_in, um, dz);
+}
+
+// Rows that do not fit registers: the differences first (FAR), one sweep with
+// the running maximum, one for the gradient.
+template <int GT>
+__global__ __launch_bounds__(1024) void k_distill_long(zo_distill a)
+{
+    using T = typename Elem<GT>::T;
+    constexpr int TH = 1024, K = Elem<GT>::kVec, NW = TH / 64;
+    extern __shared__ uint32_t bits[];
+    __shared__ DistillShared<TH> s;
+    const T *z = static_cast<const T *>(a.z) + (int64_t)blockIdx.x * a.ldz;
+    T *dz = a.dz ? static_cast<T *>(a.dz) + (int64_t)blockIdx.x * a.lddz : nullptr;
+    Row<TH> R;
+    if (!read_row<GT, TH>(a, R, s, bits, z)) {
+        skip_row<GT, TH>(a, blockIdx.x, dz);
+        return;
+    }
+    const float c = R.c;
+    float m = -INFINITY, sum = 0.0f, one = 0.0f, m_in, um;
+    slot_maxima(R, m_in, um);
+    with_form(R.form, [&](auto form) {
+        constexpr LabelForm F = decltype(form)::value;
+        for (int64_t i = (int64_t)threadIdx.x * K; i < R.V; i += TH * K) {
+            const u32x4 w = load16<GT>(z + i, R.V - i, kNegInf<GT>);
+            const uint32_t marks = marks_of<GT>(bits, i);
+            float x[K], mv = m;
+#pragma unroll
+            for (int q = 0; q < K; ++q) {
+                x[q] = marks >> q & 1 ? -INFINITY : elem_of<GT>(w, q);
+                mv = fmaxf(mv, x[q]);
+            }
+            if (mv != m) {
+                if (m != -INFINITY) {
+                    const float by = exp2_hw((m - mv) * c);
+                    sum *= by;
+                    if constexpr (F == kSquare) one *= by * by;
+                    if constexpr (F == kOwn) one *= exp2_hw((m - mv) * kLog2e);
+                }
+                m = mv;
+            }
+            const float b = base_of<true>(m, c);
+#pragma unroll
+            for (int q = 0; q < K; ++q) {
+                const float e = exp2_hw((x[q] - b) * c);
+                sum += e;
+                if constexpr (F == kSquare) one = __builtin_fmaf(e, e, one);
+                if constexpr (F == kOwn) one += exp2_hw((x[q] - b) * kLog2e);
+            }
+        }
+    });
+    group_put<OpMax>(m, s.red[0]);
+    group_put<OpMax>(m_in, s.red[1]);
+    group_put<OpMax>(um, s.red[2]);
+    __syncthreads();
+    const float m_out = group_get<OpMax, NW>(s.red[0]);
+    m_in = group_get<OpMax, NW>(s.red[1]);
+    um = group_get<OpMax, NW>(s.red[2]);
+    if (m != -INFINITY) {
+        sum *= exp2_hw((m - m_out) * c);
+        if (R.form == kSquare) one *= exp2_hw(2.0f * (m - m_out) * c);
+        if (R.form == kOwn) one *= exp2_hw((m - fmaxf(m_out, m_in)) * kLog2e);
+    }
+    const Stats t = statistics<true>(a, R, s, m_out, m_in, um, sum, one);
+    if (!dz) return;
+    float f_out, f_one;
+    rest_factors<true>(t, R.form, c, f_out, f_one);
+    with_form(R.form, [&](auto form) {
+        constexpr LabelForm F = decltype(form)::value;
+        for (int64_t i = (int64_t)threadIdx.x * K; i < R.V; i += TH * K) {
+            const u32x4 w = load16<GT>(z + i, R.V - i, kNegInf<GT>);
+            store_rest<GT>(dz, i, R.V, rest_gradient<GT, true, F>(w, i, c, t, f_out, f_one, R.y),
+                           marks_of<GT>(bits, i));
+        }
+    });
+    slot_gradient<GT, true>(R, t, a.tau, dz);
+}
+
+hipError_t launch_distill(const zo_distill &a, hipStream_t st)
+{
+    if (a.rows == 0) return hipSuccess;
+    const int gt = a.dtype == ZO_DTYPE_F16 ? GT_F16 : a.dtype == ZO_DTYPE_BF16 ? GT_BF16 : GT_F32;
+    return with_elem_type(gt, [&](auto g) {
+        constexpr int GT = decltype(g)::value;
+        const int64_t vecs = (a.vocab + Elem<GT>::kVec - 1) / Elem<GT>::kVec;
+        const uint32_t lds = (uint32_t)((a.vocab + 31) / 32 * 4);
+        const dim3 grid((uint32_t)a.rows);
+        if (vecs > 1024 * 16)
+            k_distill_long<GT><<<grid, 1024, lds, st>>>(a);
+        else if (vecs > 1024 * 8)
+            k_distill<GT, 1024, 16><<<grid, 1024, lds, st>>>(a);
+        else if (vecs > 1024 * 4)
+            k_distill<GT, 1024, 8><<<grid, 1024, lds, st>>>(a);
+        else if (vecs > 256 * 4)
+            k_distill<GT, 1024, 4><<<grid, 1024, lds, st>>>(a);
+        else
+            k_distill<GT, 256, 4><<<grid, 256, lds, st>>>(a);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace zo

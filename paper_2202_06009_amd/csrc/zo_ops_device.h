@@ -147,46 +147,98 @@ __device__ __forceinline__ uint32_t dpp(uint32_t v)
     return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xF, 0xF, true);
 }
 
-__device__ __forceinline__ float wave_max(float v)
+// Over the 64 lanes of a wave, in a fixed order, the result in every lane: four
+// steps within rows of 16 lanes, the rows' results handed on, lane 63 read.
+struct OpMax {
+    static constexpr float kNone = -INFINITY;
+    __device__ static float of(float a, float b) { return fmaxf(a, b); }
+};
+struct OpMin {
+    static constexpr float kNone = INFINITY;
+    __device__ static float of(float a, float b) { return fminf(a, b); }
+};
+struct OpSum {
+    static constexpr float kNone = 0.0f;
+    __device__ static float of(float a, float b) { return a + b; }
+};
+
+template <class OP, int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_step(float v)
 {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
+    const int o = __builtin_amdgcn_update_dpp((int)__float_as_uint(OP::kNone),
+                                              (int)__float_as_uint(v), CTRL, ROWS, 0xF, false);
+    return OP::of(v, __uint_as_float((uint32_t)o));
 }
 
-__device__ __forceinline__ float wave_sum(float v)
+template <class OP>
+__device__ __forceinline__ float wave_reduce(float v)
 {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+    v = dpp_step<OP, 0x111, 0xF>(v);   // row_shr:1, 2, 4, 8
+    v = dpp_step<OP, 0x112, 0xF>(v);
+    v = dpp_step<OP, 0x114, 0xF>(v);
+    v = dpp_step<OP, 0x118, 0xF>(v);
+    v = dpp_step<OP, 0x142, 0xA>(v);   // row_bcast:15 into rows 1 and 3
+    v = dpp_step<OP, 0x143, 0xC>(v);   // row_bcast:31 into rows 2 and 3
+    return __uint_as_float(
+        (uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
 }
 
-// Over a workgroup of NW waves; `s` is NW floats of shared memory that the
-// call may overwrite (it synchronises before and after).
-template <int NW>
-__device__ __forceinline__ float group_max(float v, float *s)
+// The first step of a reduction over a workgroup of NW waves: the wave's result
+// into s[wave].  After a barrier, group_get reads the whole.
+template <class OP>
+__device__ __forceinline__ void group_put(float v, float *s)
 {
-    v = wave_max(v);
-    __syncthreads();
+    v = wave_reduce<OP>(v);
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-    __syncthreads();
+}
+
+template <class OP, int NW>
+__device__ __forceinline__ float group_get(const float *s)
+{
     float r = s[0];
 #pragma unroll
-    for (int i = 1; i < NW; ++i) r = fmaxf(r, s[i]);
+    for (int i = 1; i < NW; ++i) r = OP::of(r, s[i]);
     return r;
 }
 
-template <int NW>
-__device__ __forceinline__ float group_sum(float v, float *s)
+// A row of at most TH * NV * kVec logits in the registers of a workgroup of TH
+// threads: thread tid holds the 16-byte vectors tid, tid + TH, ..., what lies
+// beyond the row being -infinity.  One pass over memory.
+template <int GT>
+constexpr uint32_t kNegInf = GT == GT_F32 ? 0xFF800000u : GT == GT_BF16 ? 0xFF80u : 0xFC00u;
+
+template <int GT, int TH, int NV>
+__device__ __forceinline__ void load_row(u32x4 (&w)[NV], const typename Elem<GT>::T *z, int64_t V)
 {
-    v = wave_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float r = s[0];
+    constexpr int K = Elem<GT>::kVec;
 #pragma unroll
-    for (int i = 1; i < NW; ++i) r += s[i];
-    return r;
+    for (int v = 0; v < NV; ++v) {
+        const int64_t i = (int64_t)(v * TH + (int)threadIdx.x) * K;
+        w[v] = load16<GT>(z + i, V - i, kNegInf<GT>);
+    }
+}
+
+template <int GT>
+__device__ __forceinline__ float max_of(const u32x4 &w)
+{
+    float m = elem_of<GT>(w, 0);
+#pragma unroll
+    for (int q = 1; q < Elem<GT>::kVec; ++q) m = fmaxf(m, elem_of<GT>(w, q));
+    return m;
+}
+
+// Where a sum of exponentials has its reference: 2^(z c - r) with r the largest
+// z c rounded.  z c - r is one fused operation, rounded relative to itself, and
+// r's own rounding is common to every term, so it cancels.  A largest logit of
+// -infinity gives 0: every term is then 0.
+__device__ __forceinline__ float reference(float m, float c)
+{
+    return m == -INFINITY ? 0.0f : m * c;
+}
+
+__device__ __forceinline__ float term(float z, float c, float r)
+{
+    return exp2_hw(__builtin_fmaf(z, c, -r));
 }
 
 }  // namespace zo

@@ -1,0 +1,394 @@
+// zo_top.hip -- the largest logits of every row, their columns, and the row's
+// log-sum-exp.
+//
+// One workgroup per row; the bound is reading the logits once.  A row that fits
+// the registers of the workgroup stays there (k_top); its k largest are found
+// from a bound below them: of G groups of the row, k have a maximum of at least
+// the k-th largest group maximum, so the row has at least k logits of at least
+// that, and few more when G is several times k.  The group maxima are counted in
+// 256 bins of the integer order of their bits (twice, the second time within
+// the bin that holds the k-th, when the first leaves many), the logits in and
+// above the bin found are collected, and sorted by one 64-bit key: the value's
+// order above the complement of the column, so that of equal logits the lowest
+// column comes first and no order of the collection shows.
+//
+// Rows on which this collects more than it has room for (ties, masks), rows
+// with NaN, and rows that do not fit are counted digit by digit from memory
+// (select_row): exact for everything, several reads.
+#include "zo_ops_device.h"
+
+namespace zo {
+
+// Binary32 in the order of unsigned integers: ascending, -0 as +0, NaN last.
+__device__ __forceinline__ uint32_t order_key(float v)
+{
+    uint32_t b = __float_as_uint(v);
+    if (v == 0.0f) b = 0;
+    const uint32_t k = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+    return v != v ? 0xFFFFFFFFu : k;
+}
+
+__device__ __forceinline__ float key_value(uint32_t k)
+{
+    return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+
+__device__ __forceinline__ uint64_t full_key(uint32_t key, uint32_t column)
+{
+    return (uint64_t)key << 32 | (uint32_t)~column;
+}
+
+constexpr int kRoom = 2048;      // candidates
+
+template <int TH>
+struct TopShared {
+    alignas(16) uint64_t cand[kRoom];
+    uint32_t hist[256];
+    uint32_t sel[4];
+    uint32_t wcount[TH / 64];
+    float red[4][TH / 64];
+};
+
+__device__ __forceinline__ void put_result(const TopArgs &a, int64_t row, int rank, uint64_t key)
+{
+    a.values[row * a.top + rank] = key_value((uint32_t)(key >> 32));
+    a.columns[row * a.top + rank] = (int32_t)~(uint32_t)key;
+}
+
+// The first a.top of the n keys in s.cand, in descending order, n <= kRoom.
+template <int TH>
+__device__ void sort_out(const TopArgs &a, int64_t row, TopShared<TH> &s, int n)
+{
+    const int tid = threadIdx.x;
+    if (n <= 256) {
+        // each key's rank is the number of larger keys (all differ): no barriers
+        if (tid == 0 && (n & 1)) s.cand[n] = 0;
+        __syncthreads();
+        if (tid < n) {
+            const uint64_t mine = s.cand[tid];
+            const ulong2 *p = reinterpret_cast<const ulong2 *>(s.cand);
+            int rank = 0;
+            for (int j = 0; j < (n + 1) / 2; ++j) {
+                const ulong2 o = p[j];
+                rank += (o.x > mine) + (o.y > mine);
+            }
+            if (rank < a.top) put_result(a, row, rank, mine);
+        }
+        return;
+    }
+    // bitonic, descending, over the next power of two
+    int size = 512;
+    while (size < n) size *= 2;
+    for (int i = n + tid; i < size; i += TH) s.cand[i] = 0;
+    for (int k = 2; k <= size; k *= 2)
+        for (int j = k / 2; j; j /= 2) {
+            __syncthreads();
+            for (int t = tid; t < size / 2; t += TH) {
+                const int i = 2 * t - (t & (j - 1));      // bit j of i is 0
+                const uint64_t x = s.cand[i], y = s.cand[i + j];
+                if (((i & k) == 0) == (x < y)) {
+                    s.cand[i] = y;
+                    s.cand[i + j] = x;
+                }
+            }
+        }
+    __syncthreads();
+    for (int i = tid; i < a.top; i += TH) put_result(a, row, i, s.cand[i]);
+}
+
+// The digit of the `left`-th largest key in s.hist (256 bins): s.sel[0], what is
+// then left within it in s.sel[1], and how many are in and above it in s.sel[2].
+// By the first wave, four bins a lane.
+template <int TH>
+__device__ __forceinline__ void find_bin(TopShared<TH> &s, uint32_t left)
+{
+    const int lane = threadIdx.x;
+    if (lane >= 64) return;
+    const u32x4 h = *reinterpret_cast<const u32x4 *>(s.hist + 4 * lane);
+    const uint32_t own = h[0] + h[1] + h[2] + h[3];
+    uint32_t n = own;                                   // of this lane and those above
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const uint32_t up = __shfl_down(n, o, 64);
+        if (lane + o < 64) n += up;
+    }
+    uint32_t above = n - own;
+#pragma unroll
+    for (int q = 3; q >= 0; --q) {
+        if (above < left && above + h[q] >= left) {
+            s.sel[0] = 4 * lane + q;
+            s.sel[1] = left - above;
+            s.sel[2] = above + h[q];
+        }
+        above += h[q];
+    }
+}
+
+// Any row, from memory: the k-th largest key digit by digit, the keys above it
+// and the lowest columns of those equal to it.
+template <int GT, int TH>
+__device__ void select_row(const TopArgs &a, int64_t row, TopShared<TH> &s)
+{
+    constexpr int NW = TH / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const auto *z = static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ld;
+    const int64_t V = a.vocab;
+    uint32_t prefix = 0, left = (uint32_t)a.top;
+    for (int p = 24; p >= 0; p -= 8) {
+        __syncthreads();
+        for (int i = tid; i < 256; i += TH) s.hist[i] = 0;
+        __syncthreads();
+        for (int64_t i = tid; i < V; i += TH) {
+            const uint32_t k = order_key(widen<GT>(z[i]));
+            if (((uint64_t)(k ^ prefix) >> (p + 8)) == 0) atomicAdd(&s.hist[k >> p & 255], 1u);
+        }
+        __syncthreads();
+        find_bin<TH>(s, left);
+        __syncthreads();
+        prefix |= s.sel[0] << p;
+        left = s.sel[1];
+    }
+    __syncthreads();
+    if (tid == 0) s.sel[0] = 0;
+    uint32_t equal = 0;                                  // so far
+    for (int64_t i0 = 0; i0 < V; i0 += TH) {
+        const int64_t i = i0 + tid;
+        const uint32_t k = i < V ? order_key(widen<GT>(z[i])) : 0;
+        const uint64_t mask = __ballot(i < V && k == prefix);
+        if (lane == 0) s.wcount[wave] = __popcll(mask);
+        __syncthreads();
+        if (i < V && k > prefix) s.cand[atomicAdd(&s.sel[0], 1u)] = full_key(k, (uint32_t)i);
+        uint32_t at = equal + __popcll(mask & ((1ull << lane) - 1));
+        for (int w = 0; w < NW; ++w) {
+            if (w < wave) at += s.wcount[w];
+            equal += s.wcount[w];
+        }
+        if (i < V && k == prefix && at < left)
+            s.cand[a.top - left + at] = full_key(k, (uint32_t)i);
+        __syncthreads();
+    }
+    sort_out<TH>(a, row, s, a.top);
+}
+
+// log(sum) from the pieces: largest logit m, s = sum of 2^(z c - r).
+__device__ __forceinline__ float lse_of(float m, float s, float tau, bool nan)
+{
+    if (nan) return NAN;
+    if (m == INFINITY || m == -INFINITY) return m;
+    return m / tau + logf(s);
+}
+
+// Rows that do not fit registers.
+template <int GT>
+__global__ __launch_bounds__(1024) void k_top_long(TopArgs a)
+{
+    constexpr int TH = 1024, K = Elem<GT>::kVec;
+    __shared__ TopShared<TH> s;
+    const int64_t row = blockIdx.x, V = a.vocab;
+    const auto *z = static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ld;
+    if (a.lse) {
+        // differences first, then the factor: no reference is needed beforehand
+        const float c = kLog2e / a.tau;
+        float m = -INFINITY, sum = 0.0f;
+        bool nan = false;
+        for (int64_t i = (int64_t)threadIdx.x * K; i < V; i += TH * K) {
+            const u32x4 w = load16<GT>(z + i, V - i, kNegInf<GT>);
+            const float mv = fmaxf(m, max_of<GT>(w));
+            if (mv != -INFINITY && m != mv) {
+                sum *= exp2_hw((m - mv) * c);
+                m = mv;
+            }
+#pragma unroll
+            for (int q = 0; q < K; ++q) {
+                const float v = elem_of<GT>(w, q);
+                nan |= v != v;
+                if (m != -INFINITY) sum += exp2_hw((v - m) * c);
+            }
+        }
+        group_put<OpMax>(m, s.red[0]);
+        group_put<OpMax>(nan ? 1.0f : 0.0f, s.red[1]);
+        __syncthreads();
+        const float M = group_get<OpMax, TH / 64>(s.red[0]);
+        group_put<OpSum>(m == -INFINITY ? 0.0f : sum * exp2_hw((m - M) * c), s.red[2]);
+        __syncthreads();
+        if (threadIdx.x == 0)
+            a.lse[row] = lse_of(M, group_get<OpSum, TH / 64>(s.red[2]), a.tau,
+                                group_get<OpMax, TH / 64>(s.red[1]) > 0.0f);
+    }
+    select_row<GT, TH>(a, row, s);
+}
+
+// Group maxima per thread up to this many wanted, per 16-byte vector beyond: with
+// G = 1024 groups, half as many collected logits too many are expected at k = G / 2.
+constexpr int kByThread = 256;
+
+template <int GT, int TH, int NV>
+__global__ __launch_bounds__(TH) void k_top(TopArgs a)
+{
+    constexpr int K = Elem<GT>::kVec, NW = TH / 64;
+    __shared__ TopShared<TH> s;
+    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x, V = a.vocab;
+    const auto *z = static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ld;
+    u32x4 w[NV];
+    load_row<GT, TH, NV>(w, z, V);
+    for (int i = tid; i < 256; i += TH) s.hist[i] = 0;
+    if (tid == 0) s.sel[3] = 0;
+
+    float vm[NV], m = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        vm[v] = max_of<GT>(w[v]);
+        m = fmaxf(m, vm[v]);
+    }
+    // smallest maximum of the groups that have logits
+    const int groups = (int)((V + K - 1) / K);
+    const bool by_thread = a.top <= kByThread;
+    float lo = INFINITY;
+    if (by_thread) {
+        if (tid < groups) lo = m;
+    } else {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            if (v * TH + tid < groups) lo = fminf(lo, vm[v]);
+    }
+    group_put<OpMax>(m, s.red[0]);
+    group_put<OpMin>(lo, s.red[1]);
+    __syncthreads();
+    const float M = group_get<OpMax, NW>(s.red[0]);
+    lo = group_get<OpMin, NW>(s.red[1]);
+
+    // log-sum-exp; its NaN also tells of a row with NaN (the maxima pass over it)
+    const float c = kLog2e / a.tau, r = reference(M, c);
+    const bool far = !(fabsf(r) < 0x1p126f);             // the lowest values as a mask
+    float sum = 0.0f;
+    if (far) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int q = 0; q < K; ++q) sum += exp2_hw((elem_of<GT>(w[v], q) - M) * c);
+    } else {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int q = 0; q < K; ++q) sum += term(elem_of<GT>(w[v], q), c, r);
+    }
+    group_put<OpSum>(sum, s.red[2]);
+
+    // bins of the group maxima: key - key(lo), shifted until 256 bins cover them
+    const bool all = V <= kRoom;                         // every logit is a candidate
+    const uint32_t klo = order_key(lo);
+    int shift = 32 - __clz((int)(order_key(M) - klo));
+    shift = max(0, shift - 8);
+    uint32_t least = 0;                                  // key of the lowest candidate
+    if (!all) {
+        auto count = [&](float g, bool there) {
+            const uint32_t k = order_key(g) - klo;
+            if (there) atomicAdd(&s.hist[min(k >> shift, 255u)], 1u);   // NaN: not far off
+        };
+        if (by_thread) {
+            count(m, tid < groups);
+        } else {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) count(vm[v], v * TH + tid < groups);
+        }
+        __syncthreads();
+        find_bin<TH>(s, (uint32_t)a.top);
+        __syncthreads();
+        const uint32_t bin = s.sel[0], left = s.sel[1];
+        const bool finer = shift > 0 && s.sel[2] > (uint32_t)a.top + 64;
+        least = klo + (bin << shift);
+        if (finer) {
+            __syncthreads();
+            for (int i = tid; i < 256; i += TH) s.hist[i] = 0;
+            __syncthreads();
+            const int fine = max(0, shift - 8);
+            auto again = [&](float g, bool there) {
+                const uint32_t k = order_key(g) - klo;
+                if (there && k >> shift == bin)
+                    atomicAdd(&s.hist[min((k - (bin << shift)) >> fine, 255u)], 1u);
+            };
+            if (by_thread) {
+                again(m, tid < groups);
+            } else {
+#pragma unroll
+                for (int v = 0; v < NV; ++v) again(vm[v], v * TH + tid < groups);
+            }
+            __syncthreads();
+            find_bin<TH>(s, left);
+            __syncthreads();
+            least += s.sel[0] << fine;
+        }
+    } else {
+        __syncthreads();
+    }
+    const float total = group_get<OpSum, NW>(s.red[2]);
+    if (total != total) {                                // NaN, or an infinity, is about
+        float nan = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int q = 0; q < K; ++q) {
+                const float x = elem_of<GT>(w[v], q);
+                if (x != x) nan = 1.0f;
+            }
+        group_put<OpMax>(nan, s.red[3]);
+        __syncthreads();
+        if (a.lse && tid == 0)
+            a.lse[row] = lse_of(M, total, a.tau, group_get<OpMax, NW>(s.red[3]) > 0.0f);
+        select_row<GT, TH>(a, row, s);
+        return;
+    }
+    if (a.lse && tid == 0) a.lse[row] = lse_of(M, total, a.tau, false);
+    // collect
+    const float bound = key_value(least);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        if (!all && !(vm[v] >= bound)) continue;
+        const int64_t i = (int64_t)(v * TH + tid) * K;
+        if (i >= V) continue;
+#pragma unroll
+        for (int q = 0; q < K; ++q) {
+            const float x = elem_of<GT>(w[v], q);
+            if (i + q < V && (all || x >= bound)) {
+                const uint32_t at = atomicAdd(&s.sel[3], 1u);
+                if (at < kRoom) s.cand[at] = full_key(order_key(x), (uint32_t)(i + q));
+            }
+        }
+    }
+    __syncthreads();
+    const uint32_t n = s.sel[3];
+    if (n > kRoom) {
+        select_row<GT, TH>(a, row, s);
+        return;
+    }
+    sort_out<TH>(a, row, s, (int)n);
+}
+
+template <int GT, int TH, int NV>
+static hipError_t launch_k_top(const TopArgs &a, hipStream_t st)
+{
+    k_top<GT, TH, NV><<<dim3((uint32_t)a.rows), TH, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_top_logits(const TopArgs &a, int gt, hipStream_t st)
+{
+    if (a.rows == 0) return hipSuccess;
+    return with_elem_type(gt, [&](auto g) {
+        constexpr int GT = decltype(g)::value;
+        const int64_t vecs = (a.vocab + Elem<GT>::kVec - 1) / Elem<GT>::kVec;
+        // more wanted than there are groups to bound them by
+        const bool few = a.vocab > kRoom && a.top > kByThread && a.top > vecs;
+        if (few || vecs > 1024 * 16) {
+            k_top_long<GT><<<dim3((uint32_t)a.rows), 1024, 0, st>>>(a);
+            return hipGetLastError();
+        }
+        if (a.top <= 64 && vecs <= 256 * 4) return launch_k_top<GT, 256, 4>(a, st);
+        if (vecs <= 1024 * 4) return launch_k_top<GT, 1024, 4>(a, st);
+        if (vecs <= 1024 * 8) return launch_k_top<GT, 1024, 8>(a, st);
+        return launch_k_top<GT, 1024, 16>(a, st);
+    });
+}
+
+}  // namespace zo

@@ -68,134 +68,151 @@ class Mx4:
         self._c = _Mx4(codes.data_ptr(), scales.data_ptr(), self.rows, self.cols)
 
 
-class _Call:
-    """One call's tensors: all on one device, recorded on the call's stream."""
+# The checks below read each attribute of a tensor once: a decode step calls
+# these functions for kernels of a few microseconds.
 
-    def __init__(self, where, stream):
-        self.where, self.stream, self.tensors = where, stream, []
+def _at(t, what, dev):
+    """Device pointer of t, which must be on device `dev`."""
+    if t.get_device() != dev:
+        raise ValueError(f"{what}: expected a tensor on GPU {dev}, got one on {t.device}")
+    return t.data_ptr()
 
-    def add(self, t, what):
-        if not t.is_cuda:
-            raise ValueError(f"{what}: expected a device tensor")
-        if self.tensors and t.device != self.tensors[0].device:
-            raise ValueError(f"{what}: on {t.device}, expected {self.tensors[0].device}")
-        self.tensors.append(t)
-        return t.data_ptr()
 
-    def mx4(self, q, what):
-        if not isinstance(q, Mx4):
-            raise ValueError(f"{what}: expected an Mx4")
-        self.add(q.codes, what)
-        self.add(q.scales, what)
-        return ctypes.addressof(q._c)
+def _device_of(t, what):
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{what}: expected a device tensor")
+    return dev
 
-    def matrix(self, t, what, rows=None, cols=None):
-        """(pointer, type, rows, cols, row stride)"""
-        code = _DTYPES.get(t.dtype)
-        if code is None:
-            raise ValueError(f"{what}: expected float32, float16 or bfloat16, got {t.dtype}")
-        if t.dim() != 2 or (rows is not None and tuple(t.shape) != (rows, cols)):
-            raise ValueError(f"{what}: expected shape {(rows, cols) if rows is not None else '2-d'}"
-                             f", got {tuple(t.shape)}")
-        r, c = t.shape
-        ld = t.stride(0) if r > 1 else max(c, 1)
-        if c > 1 and t.stride(1) != 1:
-            raise ValueError(f"{what}: expected contiguous rows")
-        if r > 1 and ld < c:
-            raise ValueError(f"{what}: rows overlap")
-        return self.add(t, what), code, r, c, max(ld, 1)
 
-    def vector(self, t, what, dtype, shape):
-        if t is None:
-            return None
-        if t.dtype != dtype:
-            raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
-        if tuple(t.shape) != shape or not t.is_contiguous():
-            raise ValueError(f"{what}: expected contiguous {shape}, got {tuple(t.shape)}")
-        return self.add(t, what)
+def _matrix(t, what, dev, shape=None):
+    """(pointer, element type, row stride) of a matrix with contiguous rows."""
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{what}: expected float32, float16 or bfloat16, got {t.dtype}")
+    have = t.shape
+    if len(have) != 2 or (shape is not None and tuple(have) != shape):
+        raise ValueError(f"{what}: expected shape {shape or '2-d'}, got {tuple(have)}")
+    rows, cols = have
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{what}: expected contiguous rows")
+    if rows <= 1 or cols == 0:
+        ld = max(cols, 1)
+    elif ld < cols:
+        raise ValueError(f"{what}: rows overlap")
+    return _at(t, what, dev), code, ld
 
-    def workspace(self, ws, nbytes):
-        """The caller's workspace, or one from torch's allocator on the call's stream."""
-        if nbytes == 0:
-            return None, 0
-        if ws is None:
-            dev = self.tensors[0].device
-            with torch.cuda.stream(self.stream):
-                ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        elif ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.numel() < nbytes:
-            raise ValueError(f"ws: needs {nbytes} contiguous uint8 elements")
-        return self.add(ws, "ws"), ws.numel()
 
-    def run(self, *args):
-        dev = self.tensors[0].device
-        if dev.index == torch.cuda.current_device():
-            rc = self._launch(args)
-        else:
-            with torch.cuda.device(dev):
-                rc = self._launch(args)
-        if rc != ZO_OK:
-            detail = lib().zo_ops_last_hip_error().decode() if rc == ZO_EHIP else ""
-            raise ZoError(rc, self.where, detail)
+def _vector(t, what, dev, dtype, shape):
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
+    if tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{what}: expected contiguous {shape}, got {tuple(t.shape)}")
+    return _at(t, what, dev)
 
-    def _launch(self, args):
-        current = torch.cuda.current_stream()
-        s = current if self.stream is None else self.stream
-        rc = getattr(lib(), self.where)(*args, s.cuda_stream)
-        if self.stream is not None and s != current:
-            for t in self.tensors:
-                t.record_stream(s)
-        return rc
+
+def _mx4(q, what, dev):
+    """Address of q's C struct."""
+    if not isinstance(q, Mx4):
+        raise ValueError(f"{what}: expected an Mx4")
+    if q.codes.get_device() != dev or q.scales.get_device() != dev:
+        raise ValueError(f"{what}: expected an Mx4 on GPU {dev}")
+    return ctypes.addressof(q._c)
+
+
+def _workspace(ws, nbytes, dev, stream):
+    """The caller's workspace, or one from torch's allocator on the call's stream."""
+    if nbytes == 0:
+        return None
+    if ws is None:
+        with torch.cuda.stream(stream):
+            return torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.numel() < nbytes:
+        raise ValueError(f"ws: needs {nbytes} contiguous uint8 elements")
+    _at(ws, "ws", dev)
+    return ws
+
+
+def _run(where, dev, stream, args, tensors):
+    """Calls the C function on `stream` (the current stream of GPU `dev` when None);
+    `tensors` are those that the kernels touch."""
+    f = getattr(lib(), where)
+    if dev != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _run(where, dev, stream, args, tensors)
+    current = torch._C._cuda_getCurrentRawStream(dev)
+    s = current if stream is None else stream.cuda_stream
+    rc = f(*args, s)
+    if s != current:
+        for t in tensors:
+            if isinstance(t, Mx4):
+                t.codes.record_stream(stream)
+                t.scales.record_stream(stream)
+            elif t is not None:
+                t.record_stream(stream)
+    if rc != ZO_OK:
+        detail = lib().zo_ops_last_hip_error().decode() if rc == ZO_EHIP else ""
+        raise ZoError(rc, where, detail)
 
 
 def zo_mx4_quantize(x, q=None, qt=None, stream=None):
     """x [rows, cols] into q (an Mx4 of rows x cols, blocks along x's rows) and / or
     qt (cols x rows, blocks along x's columns), reading x once."""
-    c = _Call("zo_mx4_quantize", stream)
-    p, dt, rows, cols, ld = c.matrix(x, "x")
-    c.run(p, dt, rows, cols, ld, c.mx4(q, "q") if q is not None else None,
-          c.mx4(qt, "qt") if qt is not None else None)
+    dev = _device_of(x, "x")
+    p, dt, ld = _matrix(x, "x", dev)
+    rows, cols = x.shape
+    _run("zo_mx4_quantize", dev, stream,
+         (p, dt, rows, cols, ld, None if q is None else _mx4(q, "q", dev),
+          None if qt is None else _mx4(qt, "qt", dev)), (x, q, qt))
 
 
 def zo_mx4_dequantize(q, out, stream=None):
     """The values of q into out [q.rows, q.cols]."""
-    c = _Call("zo_mx4_dequantize", stream)
-    pq = c.mx4(q, "q")
-    p, dt, _, _, ld = c.matrix(out, "out", q.rows, q.cols)
-    c.run(pq, p, dt, ld)
+    dev = _device_of(out, "out")
+    pq = _mx4(q, "q", dev)
+    p, dt, ld = _matrix(out, "out", dev, (q.rows, q.cols))
+    _run("zo_mx4_dequantize", dev, stream, (pq, p, dt, ld), (q, out))
 
 
 def zo_mx4_product(a, b, out, stream=None):
     """out [a.rows, b.rows] = a b^T, reduced over the columns of both."""
-    c = _Call("zo_mx4_product", stream)
-    pa, pb = c.mx4(a, "a"), c.mx4(b, "b")
-    p, dt, _, _, ld = c.matrix(out, "out", a.rows, b.rows)
-    c.run(pa, pb, p, dt, ld)
+    dev = _device_of(out, "out")
+    pa, pb = _mx4(a, "a", dev), _mx4(b, "b", dev)
+    p, dt, ld = _matrix(out, "out", dev, (a.rows, b.rows))
+    _run("zo_mx4_product", dev, stream, (pa, pb, p, dt, ld), (a, b, out))
 
 
 def zo_mx4_linear(x, w, out, xq, stream=None):
     """out [rows, w.rows] = x quantised along its rows times w^T; xq (an Mx4 of
     x's shape) is workspace."""
-    c = _Call("zo_mx4_linear", stream)
-    pw, pq = c.mx4(w, "w"), c.mx4(xq, "xq")
-    px, dx, rows, _, ldx = c.matrix(x, "x", xq.rows, xq.cols)
-    po, do, _, _, ldo = c.matrix(out, "out", rows, w.rows)
-    c.run(px, dx, ldx, pw, pq, po, do, ldo)
+    dev = _device_of(x, "x")
+    pw, pq = _mx4(w, "w", dev), _mx4(xq, "xq", dev)
+    px, dx, ldx = _matrix(x, "x", dev, (xq.rows, xq.cols))
+    po, do, ldo = _matrix(out, "out", dev, (xq.rows, w.rows))
+    _run("zo_mx4_linear", dev, stream, (px, dx, ldx, pw, pq, po, do, ldo), (x, w, out, xq))
 
 
 def zo_top_logits(z, values, columns, lse=None, *, tau=1.0, ws=None, stream=None):
     """The values.shape[1] largest logits of every row of z [rows, vocab] in
     descending order (ties: lowest column first) into values (float32), their
     columns into columns (int32), and log sum exp(z / tau) into lse [rows]."""
-    c = _Call("zo_top_logits", stream)
-    p, dt, rows, vocab, ld = c.matrix(z, "z")
+    dev = _device_of(z, "z")
+    p, dt, ld = _matrix(z, "z", dev)
+    rows, vocab = z.shape
     if values.dim() != 2:
         raise ValueError("values: expected a matrix")
-    shape = (rows, int(values.shape[1]))
-    pv = c.vector(values, "values", torch.float32, shape)
-    pc = c.vector(columns, "columns", torch.int32, shape)
-    pl = c.vector(lse, "lse", torch.float32, (rows,))
-    pw, nw = c.workspace(ws, zo_top_logits_ws(rows, vocab, shape[1]))
-    c.run(p, dt, rows, vocab, ld, shape[1], float(tau), pv, pc, pl, pw, nw)
+    top = values.shape[1]
+    pv = _vector(values, "values", dev, torch.float32, (rows, top))
+    pc = _vector(columns, "columns", dev, torch.int32, (rows, top))
+    pl = _vector(lse, "lse", dev, torch.float32, (rows,))
+    ws = _workspace(ws, zo_top_logits_ws(rows, vocab, top), dev, stream)
+    pw, nw = (None, 0) if ws is None else (ws.data_ptr(), ws.numel())
+    _run("zo_top_logits", dev, stream,
+         (p, dt, rows, vocab, ld, top, float(tau), pv, pc, pl, pw, nw),
+         (z, values, columns, lse, ws))
 
 
 def zo_distill_loss(z, values, columns, loss=None, dz=None, *, tau=1.0, teacher_lse=None,
@@ -210,22 +227,26 @@ def zo_distill_loss(z, values, columns, loss=None, dz=None, *, tau=1.0, teacher_
     rest of the teacher's mass as one outcome.  labels (int32 [rows], outside
     the vocabulary: none) enter with ce_weight; row_weight (float32 [rows]) is
     the gradient from above, rows of weight 0 are skipped."""
-    c = _Call("zo_distill_loss", stream)
-    p, dt, rows, vocab, ldz = c.matrix(z, "z")
+    dev = _device_of(z, "z")
+    p, dt, ldz = _matrix(z, "z", dev)
+    rows, vocab = z.shape
     if values.dim() != 2:
         raise ValueError("values: expected a matrix")
-    shape = (rows, int(values.shape[1]))
-    a = _Distill(z=p, dtype=dt, rows=rows, vocab=vocab, ldz=ldz, top=shape[1],
-                 values=c.vector(values, "values", torch.float32, shape),
-                 columns=c.vector(columns, "columns", torch.int32, shape),
-                 teacher_lse=c.vector(teacher_lse, "teacher_lse", torch.float32, (rows,)),
-                 labels=c.vector(labels, "labels", torch.int32, (rows,)),
-                 row_weight=c.vector(row_weight, "row_weight", torch.float32, (rows,)),
-                 tau=float(tau), kd_weight=float(kd_weight), ce_weight=float(ce_weight),
-                 loss=c.vector(loss, "loss", torch.float32, (rows,)))
+    top = values.shape[1]
+    pdz, lddz = None, 0
     if dz is not None:
         if dz.dtype != z.dtype:
             raise ValueError(f"dz: expected {z.dtype}, got {dz.dtype}")
-        a.dz, _, _, _, a.lddz = c.matrix(dz, "dz", rows, vocab)
-    a.ws, a.ws_bytes = c.workspace(ws, zo_distill_ws(rows, vocab))
-    c.run(ctypes.byref(a))
+        pdz, _, lddz = _matrix(dz, "dz", dev, (rows, vocab))
+    ws = _workspace(ws, zo_distill_ws(rows, vocab), dev, stream)
+    pw, nw = (None, 0) if ws is None else (ws.data_ptr(), ws.numel())
+    a = _Distill(p, dt, rows, vocab, ldz, top,
+                 _vector(values, "values", dev, torch.float32, (rows, top)),
+                 _vector(columns, "columns", dev, torch.int32, (rows, top)),
+                 _vector(teacher_lse, "teacher_lse", dev, torch.float32, (rows,)),
+                 _vector(labels, "labels", dev, torch.int32, (rows,)),
+                 _vector(row_weight, "row_weight", dev, torch.float32, (rows,)),
+                 float(tau), float(kd_weight), float(ce_weight),
+                 _vector(loss, "loss", dev, torch.float32, (rows,)), pdz, lddz, pw, nw)
+    _run("zo_distill_loss", dev, stream, (ctypes.byref(a),),
+         (z, values, columns, teacher_lse, labels, row_weight, loss, dz, ws))

@@ -110,7 +110,7 @@ def distill(z, vals, cols, *, tau=1.0, lse=None, labels=None, kd=1.0, ce=0.0, we
         inside = np.zeros(vocab, bool)
         inside[at] = True
         d, kl = np.zeros(vocab), 0.0
-        part = kd != 0 and (lse is not None or len(at) > 0)
+        part = kd != 0 and (lse is not None or (len(at) > 0 and u.max() > -np.inf))
         if part:
             if lse is None:
                 p = np.exp(u - log_sum_exp(u[None])[0])
