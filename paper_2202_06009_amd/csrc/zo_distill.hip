@@ -49,9 +49,9 @@ __device__ __forceinline__ float between(float b, float to, float c)
     return FAR ? (b - to) * c : b - to;
 }
 
-// How the label's softmax (tau = 1) follows from e: not wanted; e; e^2; by an
-// exponential of its own.
-enum LabelForm { kNoLabel, kSame, kSquare, kOwn };
+// How the label's softmax (tau = 1) follows from e: as e (and where no labels are
+// given), as e^2, by an exponential of its own.
+enum LabelForm { kSame, kSquare, kOwn };
 
 // A slot of the teacher: its column (-1: unused), the two logits, and, once the
 // row's statistics are known, the two probabilities.
@@ -75,7 +75,6 @@ struct Row {
     int32_t y;               // label, or -1
     float zy;
     bool tail;
-    LabelForm form;
     Slot slot[NS];
 };
 
@@ -88,6 +87,14 @@ struct Stats {
     float gk, ge;                       // factors of the two parts
     bool kd, none, no_rest;
 };
+
+// log2 of the exponential at tau = 1 for logit z, about the largest of all.
+template <bool FAR, LabelForm F>
+__device__ __forceinline__ float above_one(float z, float c, const Stats &t)
+{
+    if constexpr (F == kOwn) return above<FAR>(z, kLog2e, t.b_one);
+    return (F == kSquare ? 2.0f : 1.0f) * above<FAR>(z, c, t.b_all);
+}
 
 __device__ __forceinline__ bool is_marked(const uint32_t *bits, int64_t i)
 {
@@ -117,7 +124,6 @@ __device__ __forceinline__ bool read_row(const zo_distill &a, Row<TH> &R, Distil
     R.y = a.labels && a.ce_weight != 0.0f ? a.labels[R.row] : -1;
     if (R.y < 0 || R.y >= R.V) R.y = -1;
     R.zy = R.y >= 0 ? widen<GT>(z[R.y]) : 0.0f;
-    R.form = R.y < 0 ? kNoLabel : a.tau == 1.0f ? kSame : a.tau == 2.0f ? kSquare : kOwn;
     for (int i = tid; i < (int)((R.V + 31) / 32); i += TH) bits[i] = 0;
     if (tid == 0) s.dup = 0;
 #pragma unroll
@@ -155,7 +161,7 @@ __device__ __forceinline__ bool read_row(const zo_distill &a, Row<TH> &R, Distil
 // Joins the threads' sums outside S (s_out about b_out; at tau = 1: s1 about b1,
 // unless it follows from e) with the slots; writes the loss.  m_in: the slots'
 // largest logit, um the largest teacher's.  Synchronises.
-template <bool FAR, int TH>
+template <bool FAR, LabelForm F, int TH>
 __device__ __forceinline__ Stats statistics(const zo_distill &a, Row<TH> &R,
                                             DistillShared<TH> &s, float m_out, float m_in,
                                             float um, float s_out, float s1)
@@ -179,9 +185,9 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, Row<TH> &R,
         if (k.u != -INFINITY) logp[n] = (k.u - u0) / a.tau - lse;
         psum += expf(logp[n]);
         s_in += exp2_hw(above<FAR>(k.z, c, t.b_all));
-        if (R.form == kSquare)
+        if constexpr (F == kSquare)
             one_in += exp2_hw(2.0f * above<FAR>(k.z, c, t.b_all));
-        else if (R.form == kOwn)
+        else if constexpr (F == kOwn)
             one_in += exp2_hw(above<FAR>(k.z, kLog2e, t.b_one));
     }
     group_put<OpSum>(s_out, s.red[4]);
@@ -201,13 +207,12 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, Row<TH> &R,
     const float to_all = exp2_hw(log_to_all);
     t.s_all = t.s_out * to_all + s_in;
     t.share = t.none ? 0.0f : to_all / t.s_all;
-    if (R.form == kSame)
+    if constexpr (F == kSame)
         t.s_one = t.s_all;
-    else if (R.form == kSquare)
+    else if constexpr (F == kSquare)
         t.s_one = s1 * exp2_hw(2.0f * log_to_all) + one_in;
     else
         t.s_one = s1 + one_in;
-    if (R.form == kSame || R.form == kSquare) t.b_one = t.b_all;
     t.pr = 0.0f;
     if (R.tail) {
         t.pr = fmaxf(0.0f, 1.0f - psum);
@@ -249,8 +254,7 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, Row<TH> &R,
         float l = 0.0f;
         if (t.kd) l = a.kd_weight * a.tau * a.tau * kl;
         if (R.y >= 0) {
-            const float lz = R.form == kOwn ? above<FAR>(R.zy, kLog2e, t.b_one)
-                                            : above<FAR>(R.zy, c, t.b_one) * a.tau;
+            const float lz = above_one<FAR, F>(R.zy, c, t);
             l += a.ce_weight * (R.zy == -INFINITY ? INFINITY : logf(t.s_one) - lz * kLn2);
         }
         a.loss[R.row] = R.w * l;
@@ -258,97 +262,70 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, Row<TH> &R,
     return t;
 }
 
-// The gradient outside S of kVec logits from column i on, as e times the row's
+// The gradient outside S and off the label at logit z, as e times the row's
 // factors; f_out: gradient per e, f_one: the label's softmax per its exponential.
-template <int GT, bool FAR, LabelForm FORM>
-__device__ __forceinline__ u32x4 rest_gradient(const u32x4 &w, int64_t i, float c, const Stats &t,
-                                               float f_out, float f_one, int32_t y)
+template <bool FAR, LabelForm FORM>
+__device__ __forceinline__ float rest_value(float z, float c, const Stats &t, float f_out,
+                                            float f_one)
 {
-    constexpr int K = Elem<GT>::kVec;
-    float d[K];
+    const float e = exp2_hw(above<FAR>(z, c, t.b_out));
+    if constexpr (FORM == kSame)
+        return f_out * e;
+    else if constexpr (FORM == kSquare)
+        return e * __builtin_fmaf(f_one, e, f_out);
+    else
+        return __builtin_fmaf(f_out, e, f_one * exp2_hw(above<FAR>(z, kLog2e, t.b_one)));
+}
+
+// Of kVec logits.
+template <int GT, bool FAR, LabelForm FORM>
+__device__ __forceinline__ u32x4 rest_gradient(const u32x4 &w, float c, const Stats &t,
+                                               float f_out, float f_one)
+{
+    float d[Elem<GT>::kVec];
 #pragma unroll
-    for (int q = 0; q < K; ++q) {
-        const float z = elem_of<GT>(w, q);
-        const float e = exp2_hw(above<FAR>(z, c, t.b_out));
-        if constexpr (FORM == kNoLabel || FORM == kSame)
-            d[q] = f_out * e;
-        else if constexpr (FORM == kSquare)
-            d[q] = e * __builtin_fmaf(f_one, e, f_out);
-        else
-            d[q] = __builtin_fmaf(f_out, e, f_one * exp2_hw(above<FAR>(z, kLog2e, t.b_one)));
-    }
-    if constexpr (FORM != kNoLabel) {
-        const uint32_t at = (uint32_t)(y - (int32_t)i);
-        if (at < (uint32_t)K) {
-#pragma unroll
-            for (int q = 0; q < K; ++q)
-                if (at == (uint32_t)q) d[q] -= t.ge;
-        }
-    }
+    for (int q = 0; q < Elem<GT>::kVec; ++q)
+        d[q] = rest_value<FAR, FORM>(elem_of<GT>(w, q), c, t, f_out, f_one);
     return pack16<GT>(d);
 }
 
-// Stores kVec gradients of which those in S are another thread's.
-template <int GT>
-__device__ __forceinline__ void store_rest(typename Elem<GT>::T *dz, int64_t i, int64_t V,
-                                           const u32x4 &d, uint32_t marks)
-{
-    using T = typename Elem<GT>::T;
-    if (marks == 0) {
-        store16<GT>(dz + i, d, V - i);
-        return;
-    }
-#pragma unroll
-    for (int q = 0; q < Elem<GT>::kVec; ++q)
-        if (i + q < V && !(marks >> q & 1))
-            dz[i + q] = GT == GT_F32 ? (T)d[q & 3] : (T)(d[(q >> 1) & 3] >> (16 * (q & 1)));
-}
-
-// Factors of rest_gradient.
-template <bool FAR>
-__device__ __forceinline__ void rest_factors(const Stats &t, LabelForm form, float c, float &f_out,
+// Factors of rest_value.
+template <bool FAR, LabelForm F>
+__device__ __forceinline__ void rest_factors(const Stats &t, bool label, float c, float &f_out,
                                              float &f_one)
 {
     f_out = !t.kd || t.no_rest ? 0.0f : t.gk * (t.share - t.pr / t.s_out);
     f_one = 0.0f;
-    if (form == kNoLabel || t.no_rest) return;
-    if (form == kSame) {
+    if (!label || t.no_rest) return;
+    if constexpr (F == kSame)
         f_out += t.ge * t.share;
-    } else {
-        const float shift = form == kSquare ? 2.0f * between<FAR>(t.b_out, t.b_all, c) : 0.0f;
-        f_one = t.ge * exp2_hw(shift) / t.s_one;
-    }
+    else if constexpr (F == kSquare)
+        f_one = t.ge * exp2_hw(2.0f * between<FAR>(t.b_out, t.b_all, c)) / t.s_one;
+    else
+        f_one = t.ge / t.s_one;
 }
 
-// The gradient at the thread's slots.
-template <int GT, bool FAR, int TH>
-__device__ __forceinline__ void slot_gradient(const Row<TH> &R, const Stats &t, float tau,
+// The gradient at the slots and at the label, over what the sweep left there.
+// Synchronises first.
+template <int GT, bool FAR, LabelForm F, int TH>
+__device__ __forceinline__ void slot_gradient(const Row<TH> &R, const Stats &t, float f_out,
+                                              float f_one, const uint32_t *bits,
                                               typename Elem<GT>::T *dz)
 {
+    __syncthreads();
 #pragma unroll
     for (int n = 0; n < R.NS; ++n) {
         const Slot &k = R.slot[n];
         if (k.col < 0) continue;
         float d = t.kd ? t.gk * (k.q - k.p) : 0.0f;
-        if (R.form != kNoLabel) {
-            const float l = R.form == kOwn ? above<FAR>(k.z, kLog2e, t.b_one)
-                                           : above<FAR>(k.z, R.c, t.b_one) * tau;
+        if (R.y >= 0) {
+            const float l = above_one<FAR, F>(k.z, R.c, t);
             d += t.ge * ((t.none ? 0.0f : exp2_hw(l) / t.s_one) - (k.col == R.y ? 1.0f : 0.0f));
         }
         dz[k.col] = narrow<GT>(d);
     }
-}
-
-// Calls f(integral_constant<FORM>).
-template <class F>
-__device__ __forceinline__ void with_form(LabelForm form, F &&f)
-{
-    switch (form) {
-    case kNoLabel: f(std::integral_constant<LabelForm, kNoLabel>{}); break;
-    case kSame: f(std::integral_constant<LabelForm, kSame>{}); break;
-    case kSquare: f(std::integral_constant<LabelForm, kSquare>{}); break;
-    case kOwn: f(std::integral_constant<LabelForm, kOwn>{}); break;
-    }
+    if (threadIdx.x == 0 && R.y >= 0 && !is_marked(bits, R.y))
+        dz[R.y] = narrow<GT>(rest_value<FAR, F>(R.zy, R.c, t, f_out, f_one) - t.ge);
 }
 
 // The slots' largest logits.
@@ -369,153 +346,51 @@ __device__ __forceinline__ void skip_row(const zo_distill &a, int64_t row,
 {
     constexpr int K = Elem<GT>::kVec;
     if (a.loss && threadIdx.x == 0) a.loss[row] = 0.0f;
-    if (dz)
+    if (a.dz)
         for (int64_t i = (int64_t)threadIdx.x * K; i < a.vocab; i += TH * K)
             store16<GT>(dz + i, u32x4{0, 0, 0, 0}, a.vocab - i);
 }
 
-// Sums and gradient of a row in registers.
-template <int GT, int TH, int NV, bool FAR>
-__device__ __forceinline__ void resident_row(const zo_distill &a, Row<TH> &R,
-                                             DistillShared<TH> &s, const uint32_t *bits,
-                                             const u32x4 (&w)[NV], float m_out, float m_in,
-                                             float um, typename Elem<GT>::T *dz)
+// A row from memory: the differences first (FAR), one sweep with the running
+// maximum, one for the gradient.
+template <int GT, LabelForm F, int TH>
+__device__ void far_row(const zo_distill &a, Row<TH> &R, DistillShared<TH> &s,
+                        const uint32_t *bits, const typename Elem<GT>::T *z,
+                        typename Elem<GT>::T *dz)
 {
-    constexpr int K = Elem<GT>::kVec;
-    const float c = R.c, b = base_of<FAR>(m_out, c);
-    const float b1 = base_of<FAR>(fmaxf(m_out, m_in), kLog2e);
-    float sum = 0.0f, one = 0.0f;
-    with_form(R.form, [&](auto form) {
-        constexpr LabelForm F = decltype(form)::value;
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int q = 0; q < K; ++q) {
-                const float z = elem_of<GT>(w[v], q), e = exp2_hw(above<FAR>(z, c, b));
-                sum += e;
-                if constexpr (F == kSquare) one = __builtin_fmaf(e, e, one);
-                if constexpr (F == kOwn) one += exp2_hw(above<FAR>(z, kLog2e, b1));
-            }
-    });
-    const Stats t = statistics<FAR>(a, R, s, m_out, m_in, um, sum, one);
-    if (!dz) return;
-    float f_out, f_one;
-    rest_factors<FAR>(t, R.form, c, f_out, f_one);
-    with_form(R.form, [&](auto form) {
-        constexpr LabelForm F = decltype(form)::value;
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int64_t i = (int64_t)(v * TH + (int)threadIdx.x) * K;
-            if (i >= R.V) break;
-            store_rest<GT>(dz, i, R.V,
-                           rest_gradient<GT, FAR, F>(w[v], i, c, t, f_out, f_one, R.y),
-                           marks_of<GT>(bits, i));
-        }
-    });
-    slot_gradient<GT, FAR>(R, t, a.tau, dz);
-}
-
-template <int GT, int TH, int NV>
-__global__ __launch_bounds__(TH) void k_distill(zo_distill a)
-{
-    using T = typename Elem<GT>::T;
     constexpr int K = Elem<GT>::kVec, NW = TH / 64;
-    extern __shared__ uint32_t bits[];
-    __shared__ DistillShared<TH> s;
-    const T *z = static_cast<const T *>(a.z) + (int64_t)blockIdx.x * a.ldz;
-    T *dz = a.dz ? static_cast<T *>(a.dz) + (int64_t)blockIdx.x * a.lddz : nullptr;
-    Row<TH> R;
-    if (a.row_weight && a.row_weight[blockIdx.x] == 0.0f) {
-        skip_row<GT, TH>(a, blockIdx.x, dz);
-        return;
-    }
-    u32x4 w[NV];
-    load_row<GT, TH, NV>(w, z, a.vocab);      // in flight while the slots are read
-    read_row<GT, TH>(a, R, s, bits, z);
-    float m_out = -INFINITY, m_in, um;
-    slot_maxima(R, m_in, um);
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int64_t i = (int64_t)(v * TH + (int)threadIdx.x) * K;
-        const uint32_t marks = i < R.V ? marks_of<GT>(bits, i) : 0u;
-        if (marks) {
-#pragma unroll
-            for (int q = 0; q < K; ++q)
-                if (marks >> q & 1) {
-                    if constexpr (GT == GT_F32)
-                        w[v][q] = kNegInf<GT>;
-                    else
-                        w[v][q >> 1] = q & 1 ? (w[v][q >> 1] & 0xFFFFu) | kNegInf<GT> << 16
-                                             : (w[v][q >> 1] & 0xFFFF0000u) | kNegInf<GT>;
-                }
-        }
-        m_out = fmaxf(m_out, max_of<GT>(w[v]));
-    }
-    group_put<OpMax>(m_out, s.red[0]);
-    group_put<OpMax>(m_in, s.red[1]);
-    group_put<OpMax>(um, s.red[2]);
-    __syncthreads();
-    m_out = group_get<OpMax, NW>(s.red[0]);
-    m_in = group_get<OpMax, NW>(s.red[1]);
-    um = group_get<OpMax, NW>(s.red[2]);
-    // -infinity has base 0; of the others the products with both factors must be finite
-    const float lo = fminf(m_out == -INFINITY ? 0.0f : m_out, m_in == -INFINITY ? 0.0f : m_in);
-    const float size = fmaxf(fabsf(lo), fmaxf(fabsf(fmaxf(m_out, 0.0f)), fmaxf(m_in, 0.0f)));
-    if (size * fmaxf(R.c, kLog2e) < 0x1p126f)
-        resident_row<GT, TH, NV, false>(a, R, s, bits, w, m_out, m_in, um, dz);
-    else
-        resident_row<GT, TH, NV, true>(a, R, s, bits, w, m_out, m_in, um, dz);
-}
-
-// Rows that do not fit registers: the differences first (FAR), one sweep with
-// the running maximum, one for the gradient.
-template <int GT>
-__global__ __launch_bounds__(1024) void k_distill_long(zo_distill a)
-{
-    using T = typename Elem<GT>::T;
-    constexpr int TH = 1024, K = Elem<GT>::kVec, NW = TH / 64;
-    extern __shared__ uint32_t bits[];
-    __shared__ DistillShared<TH> s;
-    const T *z = static_cast<const T *>(a.z) + (int64_t)blockIdx.x * a.ldz;
-    T *dz = a.dz ? static_cast<T *>(a.dz) + (int64_t)blockIdx.x * a.lddz : nullptr;
-    Row<TH> R;
-    if (!read_row<GT, TH>(a, R, s, bits, z)) {
-        skip_row<GT, TH>(a, blockIdx.x, dz);
-        return;
-    }
     const float c = R.c;
     float m = -INFINITY, sum = 0.0f, one = 0.0f, m_in, um;
     slot_maxima(R, m_in, um);
-    with_form(R.form, [&](auto form) {
-        constexpr LabelForm F = decltype(form)::value;
-        for (int64_t i = (int64_t)threadIdx.x * K; i < R.V; i += TH * K) {
-            const u32x4 w = load16<GT>(z + i, R.V - i, kNegInf<GT>);
-            const uint32_t marks = marks_of<GT>(bits, i);
-            float x[K], mv = m;
+    // the row's last logits count as a vector filled up with -infinity
+    for (int64_t i = (int64_t)threadIdx.x * K; i < R.V; i += TH * K) {
+        const u32x4 w = load16<GT>(z + i, R.V - i, kNegInf<GT> & kElemMask<GT>);
+        const uint32_t marks = marks_of<GT>(bits, i);
+        float x[K], mv = m;
 #pragma unroll
-            for (int q = 0; q < K; ++q) {
-                x[q] = marks >> q & 1 ? -INFINITY : elem_of<GT>(w, q);
-                mv = fmaxf(mv, x[q]);
-            }
-            if (mv != m) {
-                if (m != -INFINITY) {
-                    const float by = exp2_hw((m - mv) * c);
-                    sum *= by;
-                    if constexpr (F == kSquare) one *= by * by;
-                    if constexpr (F == kOwn) one *= exp2_hw((m - mv) * kLog2e);
-                }
-                m = mv;
-            }
-            const float b = base_of<true>(m, c);
-#pragma unroll
-            for (int q = 0; q < K; ++q) {
-                const float e = exp2_hw((x[q] - b) * c);
-                sum += e;
-                if constexpr (F == kSquare) one = __builtin_fmaf(e, e, one);
-                if constexpr (F == kOwn) one += exp2_hw((x[q] - b) * kLog2e);
-            }
+        for (int q = 0; q < K; ++q) {
+            x[q] = marks >> q & 1 ? -INFINITY : elem_of<GT>(w, q);
+            mv = fmaxf(mv, x[q]);
         }
-    });
+        if (mv != m) {
+            if (m != -INFINITY) {
+                const float by = exp2_hw((m - mv) * c);
+                sum *= by;
+                if constexpr (F == kSquare) one *= by * by;
+                if constexpr (F == kOwn) one *= exp2_hw((m - mv) * kLog2e);
+            }
+            m = mv;
+        }
+        const float b = base_of<true>(m, c);
+#pragma unroll
+        for (int q = 0; q < K; ++q) {
+            const float e = exp2_hw((x[q] - b) * c);
+            sum += e;
+            if constexpr (F == kSquare) one = __builtin_fmaf(e, e, one);
+            if constexpr (F == kOwn) one += exp2_hw((x[q] - b) * kLog2e);
+        }
+    }
+    __syncthreads();
     group_put<OpMax>(m, s.red[0]);
     group_put<OpMax>(m_in, s.red[1]);
     group_put<OpMax>(um, s.red[2]);
@@ -525,43 +400,165 @@ __global__ __launch_bounds__(1024) void k_distill_long(zo_distill a)
     um = group_get<OpMax, NW>(s.red[2]);
     if (m != -INFINITY) {
         sum *= exp2_hw((m - m_out) * c);
-        if (R.form == kSquare) one *= exp2_hw(2.0f * (m - m_out) * c);
-        if (R.form == kOwn) one *= exp2_hw((m - fmaxf(m_out, m_in)) * kLog2e);
+        if constexpr (F == kSquare) one *= exp2_hw(2.0f * (m - m_out) * c);
+        if constexpr (F == kOwn) one *= exp2_hw((m - fmaxf(m_out, m_in)) * kLog2e);
     }
-    const Stats t = statistics<true>(a, R, s, m_out, m_in, um, sum, one);
-    if (!dz) return;
+    const Stats t = statistics<true, F>(a, R, s, m_out, m_in, um, sum, one);
+    if (!a.dz) return;
     float f_out, f_one;
-    rest_factors<true>(t, R.form, c, f_out, f_one);
-    with_form(R.form, [&](auto form) {
-        constexpr LabelForm F = decltype(form)::value;
-        for (int64_t i = (int64_t)threadIdx.x * K; i < R.V; i += TH * K) {
-            const u32x4 w = load16<GT>(z + i, R.V - i, kNegInf<GT>);
-            store_rest<GT>(dz, i, R.V, rest_gradient<GT, true, F>(w, i, c, t, f_out, f_one, R.y),
-                           marks_of<GT>(bits, i));
+    rest_factors<true, F>(t, R.y >= 0, c, f_out, f_one);
+    for (int64_t i = (int64_t)threadIdx.x * K; i < R.V; i += TH * K) {
+        const u32x4 w = load16<GT>(z + i, R.V - i, kNegInf<GT> & kElemMask<GT>);
+        store16<GT>(dz + i, rest_gradient<GT, true, F>(w, c, t, f_out, f_one), R.V - i);
+    }
+    slot_gradient<GT, true, F>(R, t, f_out, f_one, bits, dz);
+}
+
+template <int GT, LabelForm F>
+__global__ __launch_bounds__(1024) void k_distill_long(zo_distill a)
+{
+    using T = typename Elem<GT>::T;
+    constexpr int TH = 1024;
+    extern __shared__ uint32_t bits[];
+    __shared__ DistillShared<TH> s;
+    const T *z = static_cast<const T *>(a.z) + (int64_t)blockIdx.x * a.ldz;
+    T *dz = static_cast<T *>(a.dz) + (int64_t)blockIdx.x * a.lddz;   // if a.dz
+    Row<TH> R;
+    if (!read_row<GT, TH>(a, R, s, bits, z)) {
+        skip_row<GT, TH>(a, blockIdx.x, dz);
+        return;
+    }
+    far_row<GT, F, TH>(a, R, s, bits, z, dz);
+}
+
+// One logit's e and its share of the sum at tau = 1.
+template <LabelForm F>
+__device__ __forceinline__ void add_terms(float z, float c, float b, float b1, float &sum,
+                                          float &one)
+{
+    const float e = exp2_hw(above<false>(z, c, b));
+    sum += e;
+    if constexpr (F == kSquare) one = __builtin_fmaf(e, e, one);
+    if constexpr (F == kOwn) one += exp2_hw(above<false>(z, kLog2e, b1));
+}
+
+template <int GT, LabelForm F, int TH, int NV>
+__global__ __launch_bounds__(TH, 4) void k_distill(zo_distill a)
+{
+    using T = typename Elem<GT>::T;
+    constexpr int K = Elem<GT>::kVec, NW = TH / 64;
+    extern __shared__ uint32_t bits[];
+    __shared__ DistillShared<TH> s;
+    const T *z = static_cast<const T *>(a.z) + (int64_t)blockIdx.x * a.ldz;
+    T *dz = static_cast<T *>(a.dz) + (int64_t)blockIdx.x * a.lddz;   // if a.dz
+    Row<TH> R;
+    if (a.row_weight && a.row_weight[blockIdx.x] == 0.0f) {
+        skip_row<GT, TH>(a, blockIdx.x, dz);
+        return;
+    }
+    Resident<GT, TH, NV> x;
+    x.load(z, a.vocab);                       // in flight while the slots are read
+    read_row<GT, TH>(a, R, s, bits, z);
+    float m_in, um;
+    slot_maxima(R, m_in, um);
+    if (x.has_last(R.V) && is_marked(bits, x.last_column())) x.last = -INFINITY;
+    float m_out = x.last;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const uint32_t marks = x.at(v) < x.vecs ? marks_of<GT>(bits, x.at(v) * K) : 0u;
+        if (marks) {
+#pragma unroll
+            for (int q = 0; q < K; ++q)
+                if (marks >> q & 1) {
+                    if constexpr (GT == GT_F32)
+                        x.w[v][q] = kNegInf<GT>;
+                    else
+                        x.w[v][q >> 1] = q & 1 ? (x.w[v][q >> 1] & 0xFFFFu) | kNegInf<GT> << 16
+                                               : (x.w[v][q >> 1] & 0xFFFF0000u) |
+                                                     (kNegInf<GT> & 0xFFFFu);
+                }
         }
-    });
-    slot_gradient<GT, true>(R, t, a.tau, dz);
+        m_out = fmaxf(m_out, max_of<GT>(x.w[v]));
+        __builtin_amdgcn_sched_barrier(0);       // keeps the unpacked logits few
+    }
+    group_put<OpMax>(m_out, s.red[0]);
+    group_put<OpMax>(m_in, s.red[1]);
+    group_put<OpMax>(um, s.red[2]);
+    __syncthreads();
+    m_out = group_get<OpMax, NW>(s.red[0]);
+    m_in = group_get<OpMax, NW>(s.red[1]);
+    um = group_get<OpMax, NW>(s.red[2]);
+    // the products of both largest logits (-infinity: none) with both factors are finite
+    const float size = fmaxf(m_out == -INFINITY ? 0.0f : fabsf(m_out),
+                             m_in == -INFINITY ? 0.0f : fabsf(m_in));
+    if (!(size * fmaxf(R.c, kLog2e) < 0x1p126f)) {
+        far_row<GT, F, TH>(a, R, s, bits, z, dz);
+        return;
+    }
+    const float c = R.c, b = base_of<false>(m_out, c);
+    const float b1 = base_of<false>(fmaxf(m_out, m_in), kLog2e);
+    float sum = 0.0f, one = 0.0f;
+    add_terms<F>(x.last, c, b, b1, sum, one);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        repack<GT>(x.w[v]);
+        if (v * TH < x.vecs) {                   // the same for all threads
+#pragma unroll
+            for (int q = 0; q < K; ++q)
+                add_terms<F>(elem_of<GT>(x.w[v], q), c, b, b1, sum, one);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    const Stats t = statistics<false, F>(a, R, s, m_out, m_in, um, sum, one);
+    if (!a.dz) return;
+    float f_out, f_one;
+    rest_factors<false, F>(t, R.y >= 0, c, f_out, f_one);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        repack<GT>(x.w[v]);
+        if (x.at(v) < x.vecs)
+            *reinterpret_cast<u32x4_a2 *>(dz + (int64_t)x.at(v) * K) =
+                rest_gradient<GT, false, F>(x.w[v], c, t, f_out, f_one);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (x.has_last(R.V))
+        dz[x.last_column()] = narrow<GT>(rest_value<false, F>(x.last, c, t, f_out, f_one));
+    slot_gradient<GT, false, F>(R, t, f_out, f_one, bits, dz);
+}
+
+template <int GT, LabelForm F>
+static void launch_form(const zo_distill &a, hipStream_t st)
+{
+    const int64_t vecs = a.vocab / Elem<GT>::kVec;
+    const uint32_t lds = (uint32_t)((a.vocab + 31) / 32 * 4);
+    const dim3 grid((uint32_t)a.rows);
+    if (vecs > 1024 * 16)
+        k_distill_long<GT, F><<<grid, 1024, lds, st>>>(a);
+    else if (vecs > 512 * 16)
+        k_distill<GT, F, 1024, 16><<<grid, 1024, lds, st>>>(a);
+    else if (vecs > 512 * 8)
+        k_distill<GT, F, 512, 16><<<grid, 512, lds, st>>>(a);
+    else if (vecs > 256 * 8)
+        k_distill<GT, F, 512, 8><<<grid, 512, lds, st>>>(a);
+    else if (vecs > 256 * 4)
+        k_distill<GT, F, 256, 8><<<grid, 256, lds, st>>>(a);
+    else
+        k_distill<GT, F, 256, 4><<<grid, 256, lds, st>>>(a);
 }
 
 hipError_t launch_distill(const zo_distill &a, hipStream_t st)
 {
     if (a.rows == 0) return hipSuccess;
     const int gt = a.dtype == ZO_DTYPE_F16 ? GT_F16 : a.dtype == ZO_DTYPE_BF16 ? GT_BF16 : GT_F32;
+    const bool labels = a.labels && a.ce_weight != 0.0f;
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
-        const int64_t vecs = (a.vocab + Elem<GT>::kVec - 1) / Elem<GT>::kVec;
-        const uint32_t lds = (uint32_t)((a.vocab + 31) / 32 * 4);
-        const dim3 grid((uint32_t)a.rows);
-        if (vecs > 1024 * 16)
-            k_distill_long<GT><<<grid, 1024, lds, st>>>(a);
-        else if (vecs > 1024 * 8)
-            k_distill<GT, 1024, 16><<<grid, 1024, lds, st>>>(a);
-        else if (vecs > 1024 * 4)
-            k_distill<GT, 1024, 8><<<grid, 1024, lds, st>>>(a);
-        else if (vecs > 256 * 4)
-            k_distill<GT, 1024, 4><<<grid, 1024, lds, st>>>(a);
+        if (!labels || a.tau == 1.0f)
+            launch_form<GT, kSame>(a, st);
+        else if (a.tau == 2.0f)
+            launch_form<GT, kSquare>(a, st);
         else
-            k_distill<GT, 256, 4><<<grid, 256, lds, st>>>(a);
+            launch_form<GT, kOwn>(a, st);
         return hipGetLastError();
     });
 }

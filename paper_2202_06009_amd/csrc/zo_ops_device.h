@@ -201,22 +201,41 @@ __device__ __forceinline__ float group_get(const float *s)
     return r;
 }
 
-// A row of at most TH * NV * kVec logits in the registers of a workgroup of TH
-// threads: thread tid holds the 16-byte vectors tid, tid + TH, ..., what lies
-// beyond the row being -infinity.  One pass over memory.
+// A row of V < TH * NV * kVec + kVec logits in the registers of a workgroup of TH
+// threads: thread tid holds the whole 16-byte vectors tid, tid + TH, ... of the
+// row (-infinity where there are no more) and the first threads one each of the
+// V % kVec logits that are left.  One pass over memory.
 template <int GT>
-constexpr uint32_t kNegInf = GT == GT_F32 ? 0xFF800000u : GT == GT_BF16 ? 0xFF80u : 0xFC00u;
+constexpr uint32_t kNegInf = GT == GT_F32 ? 0xFF800000u : GT == GT_BF16 ? 0xFF80FF80u : 0xFC00FC00u;
+
+template <int GT>
+constexpr uint32_t kElemMask = GT == GT_F32 ? 0xFFFFFFFFu : 0xFFFFu;
 
 template <int GT, int TH, int NV>
-__device__ __forceinline__ void load_row(u32x4 (&w)[NV], const typename Elem<GT>::T *z, int64_t V)
-{
-    constexpr int K = Elem<GT>::kVec;
+struct Resident {
+    static constexpr int K = Elem<GT>::kVec;
+    using T = typename Elem<GT>::T;
+    u32x4 w[NV];
+    float last;              // this thread's logit of the rest, or -infinity
+    int vecs;                // whole vectors of the row
+
+    __device__ __forceinline__ void load(const T *z, int64_t V)
+    {
+        vecs = (int)(V / K);
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int64_t i = (int64_t)(v * TH + (int)threadIdx.x) * K;
-        w[v] = load16<GT>(z + i, V - i, kNegInf<GT>);
+        for (int v = 0; v < NV; ++v) {
+            const int i = at(v);
+            w[v] = u32x4{kNegInf<GT>, kNegInf<GT>, kNegInf<GT>, kNegInf<GT>};
+            if (i < vecs) w[v] = *reinterpret_cast<const u32x4_a2 *>(z + (int64_t)i * K);
+        }
+        last = -INFINITY;
+        if ((int)threadIdx.x < (int)(V % K)) last = widen<GT>(z[last_column()]);
     }
-}
+    // Index of this thread's vector v, and column of its last logit.
+    __device__ __forceinline__ int at(int v) const { return v * TH + (int)threadIdx.x; }
+    __device__ __forceinline__ int last_column() const { return vecs * K + (int)threadIdx.x; }
+    __device__ __forceinline__ bool has_last(int64_t V) const { return last_column() < V; }
+};
 
 template <int GT>
 __device__ __forceinline__ float max_of(const u32x4 &w)
@@ -225,6 +244,15 @@ __device__ __forceinline__ float max_of(const u32x4 &w)
 #pragma unroll
     for (int q = 1; q < Elem<GT>::kVec; ++q) m = fmaxf(m, elem_of<GT>(w, q));
     return m;
+}
+
+// The compiler takes w for changed here: what is unpacked from it before is not
+// kept for later (a resident row unpacked would not fit the registers).
+template <int GT>
+__device__ __forceinline__ void repack(u32x4 &w)
+{
+    if constexpr (GT != GT_F32)
+        asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));
 }
 
 // Where a sum of exponentials has its reference: 2^(z c - r) with r the largest

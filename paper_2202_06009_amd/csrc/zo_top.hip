@@ -178,142 +178,139 @@ __device__ __forceinline__ float lse_of(float m, float s, float tau, bool nan)
     return m / tau + logf(s);
 }
 
+// The log-sum-exp of any row, from memory: the differences first, then the
+// factor, so that no product overflows and no reference is needed beforehand.
+template <int GT, int TH>
+__device__ void lse_row(const TopArgs &a, int64_t row, TopShared<TH> &s)
+{
+    constexpr int K = Elem<GT>::kVec;
+    const int64_t V = a.vocab;
+    const auto *z = static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ld;
+    const float c = kLog2e / a.tau;
+    float m = -INFINITY, sum = 0.0f;
+    bool nan = false;
+    for (int64_t i = (int64_t)threadIdx.x * K; i < V; i += TH * K) {
+        const u32x4 w = load16<GT>(z + i, V - i, kNegInf<GT> & kElemMask<GT>);
+        const float mv = fmaxf(m, max_of<GT>(w));
+        if (m != mv) {
+            sum *= m == -INFINITY ? 0.0f : exp2_hw((m - mv) * c);
+            m = mv;
+        }
+#pragma unroll
+        for (int q = 0; q < K; ++q) {
+            const float v = elem_of<GT>(w, q);
+            nan |= v != v;
+            if (m != -INFINITY) sum += exp2_hw((v - m) * c);
+        }
+    }
+    __syncthreads();
+    group_put<OpMax>(m, s.red[0]);
+    group_put<OpMax>(nan ? 1.0f : 0.0f, s.red[1]);
+    __syncthreads();
+    const float M = group_get<OpMax, TH / 64>(s.red[0]);
+    group_put<OpSum>(m == -INFINITY ? 0.0f : sum * exp2_hw((m - M) * c), s.red[2]);
+    __syncthreads();
+    if (threadIdx.x == 0)
+        a.lse[row] = lse_of(M, group_get<OpSum, TH / 64>(s.red[2]), a.tau,
+                            group_get<OpMax, TH / 64>(s.red[1]) > 0.0f);
+}
+
 // Rows that do not fit registers.
 template <int GT>
 __global__ __launch_bounds__(1024) void k_top_long(TopArgs a)
 {
-    constexpr int TH = 1024, K = Elem<GT>::kVec;
-    __shared__ TopShared<TH> s;
-    const int64_t row = blockIdx.x, V = a.vocab;
-    const auto *z = static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ld;
-    if (a.lse) {
-        // differences first, then the factor: no reference is needed beforehand
-        const float c = kLog2e / a.tau;
-        float m = -INFINITY, sum = 0.0f;
-        bool nan = false;
-        for (int64_t i = (int64_t)threadIdx.x * K; i < V; i += TH * K) {
-            const u32x4 w = load16<GT>(z + i, V - i, kNegInf<GT>);
-            const float mv = fmaxf(m, max_of<GT>(w));
-            if (mv != -INFINITY && m != mv) {
-                sum *= exp2_hw((m - mv) * c);
-                m = mv;
-            }
-#pragma unroll
-            for (int q = 0; q < K; ++q) {
-                const float v = elem_of<GT>(w, q);
-                nan |= v != v;
-                if (m != -INFINITY) sum += exp2_hw((v - m) * c);
-            }
-        }
-        group_put<OpMax>(m, s.red[0]);
-        group_put<OpMax>(nan ? 1.0f : 0.0f, s.red[1]);
-        __syncthreads();
-        const float M = group_get<OpMax, TH / 64>(s.red[0]);
-        group_put<OpSum>(m == -INFINITY ? 0.0f : sum * exp2_hw((m - M) * c), s.red[2]);
-        __syncthreads();
-        if (threadIdx.x == 0)
-            a.lse[row] = lse_of(M, group_get<OpSum, TH / 64>(s.red[2]), a.tau,
-                                group_get<OpMax, TH / 64>(s.red[1]) > 0.0f);
-    }
-    select_row<GT, TH>(a, row, s);
+    __shared__ TopShared<1024> s;
+    if (a.lse) lse_row<GT, 1024>(a, blockIdx.x, s);
+    select_row<GT, 1024>(a, blockIdx.x, s);
 }
 
-// Group maxima per thread up to this many wanted, per 16-byte vector beyond: with
-// G = 1024 groups, half as many collected logits too many are expected at k = G / 2.
-constexpr int kByThread = 256;
+// Groups of the vectors of a thread, when more than a quarter as many logits are
+// wanted as there are threads.
+constexpr int kGroups = 4;
 
 template <int GT, int TH, int NV>
-__global__ __launch_bounds__(TH) void k_top(TopArgs a)
+__global__ __launch_bounds__(TH, 4) void k_top(TopArgs a)
 {
     constexpr int K = Elem<GT>::kVec, NW = TH / 64;
     __shared__ TopShared<TH> s;
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x, V = a.vocab;
-    const auto *z = static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ld;
-    u32x4 w[NV];
-    load_row<GT, TH, NV>(w, z, V);
+    Resident<GT, TH, NV> x;
+    x.load(static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ld, V);
     for (int i = tid; i < 256; i += TH) s.hist[i] = 0;
     if (tid == 0) s.sel[3] = 0;
 
-    float vm[NV], m = -INFINITY;
+    // groups: the threads that have logits, or kGroups of every thread's vectors
+    const bool by_thread = a.top <= TH / kGroups;
+    const bool mine = tid < x.vecs || x.has_last(V);
+    float m = x.last, lo = INFINITY, gm[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) gm[g] = -INFINITY;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        vm[v] = max_of<GT>(w[v]);
-        m = fmaxf(m, vm[v]);
+        if (v * TH < x.vecs) {                           // the same for all threads
+            gm[v % kGroups] = fmaxf(gm[v % kGroups], max_of<GT>(x.w[v]));
+        }
+        __builtin_amdgcn_sched_barrier(0);
     }
-    // smallest maximum of the groups that have logits
-    const int groups = (int)((V + K - 1) / K);
-    const bool by_thread = a.top <= kByThread;
-    float lo = INFINITY;
-    if (by_thread) {
-        if (tid < groups) lo = m;
-    } else {
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
-            if (v * TH + tid < groups) lo = fminf(lo, vm[v]);
+    for (int g = 0; g < kGroups; ++g) {
+        m = fmaxf(m, gm[g]);
+        if (x.at(g) < x.vecs) lo = fminf(lo, gm[g]);
     }
+    if (by_thread) lo = mine ? m : INFINITY;
     group_put<OpMax>(m, s.red[0]);
     group_put<OpMin>(lo, s.red[1]);
     __syncthreads();
     const float M = group_get<OpMax, NW>(s.red[0]);
     lo = group_get<OpMin, NW>(s.red[1]);
 
-    // log-sum-exp; its NaN also tells of a row with NaN (the maxima pass over it)
+    // sum of 2^(c z - r); its NaN also tells of a row with NaN or +infinity (the
+    // maxima pass over NaN)
     const float c = kLog2e / a.tau, r = reference(M, c);
-    const bool far = !(fabsf(r) < 0x1p126f);             // the lowest values as a mask
-    float sum = 0.0f;
-    if (far) {
+    float sum = term(x.last, c, r);
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < NV; ++v) {
+        repack<GT>(x.w[v]);
+        if (v * TH < x.vecs) {
 #pragma unroll
-            for (int q = 0; q < K; ++q) sum += exp2_hw((elem_of<GT>(w[v], q) - M) * c);
-    } else {
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int q = 0; q < K; ++q) sum += term(elem_of<GT>(w[v], q), c, r);
+            for (int q = 0; q < K; ++q) sum += term(elem_of<GT>(x.w[v], q), c, r);
+        }
+        __builtin_amdgcn_sched_barrier(0);
     }
     group_put<OpSum>(sum, s.red[2]);
 
     // bins of the group maxima: key - key(lo), shifted until 256 bins cover them
     const bool all = V <= kRoom;                         // every logit is a candidate
-    const uint32_t klo = order_key(lo);
-    int shift = 32 - __clz((int)(order_key(M) - klo));
-    shift = max(0, shift - 8);
     uint32_t least = 0;                                  // key of the lowest candidate
     if (!all) {
-        auto count = [&](float g, bool there) {
-            const uint32_t k = order_key(g) - klo;
-            if (there) atomicAdd(&s.hist[min(k >> shift, 255u)], 1u);   // NaN: not far off
+        const uint32_t klo = order_key(lo);
+        const int shift = max(0, 24 - __clz((int)(order_key(M) - klo)));
+        const int fine = max(0, shift - 8);
+        auto count = [&](float g, bool there, uint32_t from, int by, uint32_t bins) {
+            const uint32_t k = (order_key(g) - from) >> by;
+            if (there && k < bins) atomicAdd(&s.hist[k], 1u);
         };
-        if (by_thread) {
-            count(m, tid < groups);
-        } else {
+        auto count_all = [&](uint32_t from, int by, uint32_t bins) {
+            if (by_thread) {
+                count(m, mine, from, by, bins);
+            } else {
 #pragma unroll
-            for (int v = 0; v < NV; ++v) count(vm[v], v * TH + tid < groups);
-        }
+                for (int g = 0; g < kGroups; ++g)
+                    count(gm[g], x.at(g) < x.vecs, from, by, bins);
+            }
+        };
+        count_all(klo, shift, 256);
         __syncthreads();
         find_bin<TH>(s, (uint32_t)a.top);
         __syncthreads();
-        const uint32_t bin = s.sel[0], left = s.sel[1];
-        const bool finer = shift > 0 && s.sel[2] > (uint32_t)a.top + 64;
-        least = klo + (bin << shift);
-        if (finer) {
+        const uint32_t left = s.sel[1];
+        least = klo + (s.sel[0] << shift);
+        if (shift > 0 && s.sel[2] > (uint32_t)a.top + 64) {
             __syncthreads();
             for (int i = tid; i < 256; i += TH) s.hist[i] = 0;
             __syncthreads();
-            const int fine = max(0, shift - 8);
-            auto again = [&](float g, bool there) {
-                const uint32_t k = order_key(g) - klo;
-                if (there && k >> shift == bin)
-                    atomicAdd(&s.hist[min((k - (bin << shift)) >> fine, 255u)], 1u);
-            };
-            if (by_thread) {
-                again(m, tid < groups);
-            } else {
-#pragma unroll
-                for (int v = 0; v < NV; ++v) again(vm[v], v * TH + tid < groups);
-            }
+            count_all(least, fine, 1u << (shift - fine));
             __syncthreads();
             find_bin<TH>(s, left);
             __syncthreads();
@@ -323,38 +320,29 @@ __global__ __launch_bounds__(TH) void k_top(TopArgs a)
         __syncthreads();
     }
     const float total = group_get<OpSum, NW>(s.red[2]);
-    if (total != total) {                                // NaN, or an infinity, is about
-        float nan = 0.0f;
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int q = 0; q < K; ++q) {
-                const float x = elem_of<GT>(w[v], q);
-                if (x != x) nan = 1.0f;
-            }
-        group_put<OpMax>(nan, s.red[3]);
-        __syncthreads();
-        if (a.lse && tid == 0)
-            a.lse[row] = lse_of(M, total, a.tau, group_get<OpMax, NW>(s.red[3]) > 0.0f);
+    if (total != total || !(fabsf(r) < 0x1p126f)) {      // or c z near overflow
+        if (a.lse) lse_row<GT, TH>(a, row, s);
         select_row<GT, TH>(a, row, s);
         return;
     }
     if (a.lse && tid == 0) a.lse[row] = lse_of(M, total, a.tau, false);
     // collect
     const float bound = key_value(least);
+    auto offer = [&](float z, int i) {
+        if (all || z >= bound) {
+            const uint32_t at = atomicAdd(&s.sel[3], 1u);
+            if (at < kRoom) s.cand[at] = full_key(order_key(z), (uint32_t)i);
+        }
+    };
+    if (x.has_last(V)) offer(x.last, x.last_column());
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        if (!all && !(vm[v] >= bound)) continue;
-        const int64_t i = (int64_t)(v * TH + tid) * K;
-        if (i >= V) continue;
+        repack<GT>(x.w[v]);
+        if (x.at(v) < x.vecs && (all || max_of<GT>(x.w[v]) >= bound)) {
 #pragma unroll
-        for (int q = 0; q < K; ++q) {
-            const float x = elem_of<GT>(w[v], q);
-            if (i + q < V && (all || x >= bound)) {
-                const uint32_t at = atomicAdd(&s.sel[3], 1u);
-                if (at < kRoom) s.cand[at] = full_key(order_key(x), (uint32_t)(i + q));
-            }
+            for (int q = 0; q < K; ++q) offer(elem_of<GT>(x.w[v], q), x.at(v) * K + q);
         }
+        __builtin_amdgcn_sched_barrier(0);
     }
     __syncthreads();
     const uint32_t n = s.sel[3];
@@ -377,16 +365,18 @@ hipError_t launch_top_logits(const TopArgs &a, int gt, hipStream_t st)
     if (a.rows == 0) return hipSuccess;
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
-        const int64_t vecs = (a.vocab + Elem<GT>::kVec - 1) / Elem<GT>::kVec;
-        // more wanted than there are groups to bound them by
-        const bool few = a.vocab > kRoom && a.top > kByThread && a.top > vecs;
+        const int64_t vecs = a.vocab / Elem<GT>::kVec;
+        // few: fewer groups with logits than are wanted bound nothing
+        const bool few = a.vocab > kRoom && a.top > 64 && a.top > vecs;
         if (few || vecs > 1024 * 16) {
             k_top_long<GT><<<dim3((uint32_t)a.rows), 1024, 0, st>>>(a);
             return hipGetLastError();
         }
-        if (a.top <= 64 && vecs <= 256 * 4) return launch_k_top<GT, 256, 4>(a, st);
-        if (vecs <= 1024 * 4) return launch_k_top<GT, 1024, 4>(a, st);
-        if (vecs <= 1024 * 8) return launch_k_top<GT, 1024, 8>(a, st);
+        // the more are wanted, the more groups: about 4 a logit or more
+        if (a.top <= 256 && vecs <= 256 * 4) return launch_k_top<GT, 256, 4>(a, st);
+        if (a.top <= 256 && vecs <= 256 * 8) return launch_k_top<GT, 256, 8>(a, st);
+        if (a.top <= 512 && vecs <= 512 * 8) return launch_k_top<GT, 512, 8>(a, st);
+        if (a.top <= 512 && vecs <= 512 * 16) return launch_k_top<GT, 512, 16>(a, st);
         return launch_k_top<GT, 1024, 16>(a, st);
     });
 }
