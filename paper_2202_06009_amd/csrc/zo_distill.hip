@@ -76,6 +76,14 @@ struct Row {
     float zy;
     bool tail;
     Slot slot[NS];
+    // Calls f(slot) for the thread's used slots; waves without one skip it.
+    template <class F>
+    __device__ __forceinline__ void slots(F &&f)
+    {
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+            if (__ballot(slot[n].col >= 0) != 0 && slot[n].col >= 0) f(slot[n], n);
+    }
 };
 
 // What a row's gradient follows from, besides its logits.
@@ -177,11 +185,8 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, Row<TH> &R,
     t.kd = a.kd_weight != 0.0f && (R.tail || um != -INFINITY);
     const float lse = R.tail ? a.teacher_lse[R.row] : 0.0f, u0 = R.tail ? 0.0f : um;
     float logp[Row<TH>::NS], s_in = 0.0f, one_in = 0.0f, psum = 0.0f;
-#pragma unroll
-    for (int n = 0; n < R.NS; ++n) {
-        const Slot &k = R.slot[n];
+    R.slots([&](Slot &k, int n) {
         logp[n] = -INFINITY;
-        if (k.col < 0) continue;
         if (k.u != -INFINITY) logp[n] = (k.u - u0) / a.tau - lse;
         psum += expf(logp[n]);
         s_in += exp2_hw(above<FAR>(k.z, c, t.b_all));
@@ -189,7 +194,7 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, Row<TH> &R,
             one_in += exp2_hw(2.0f * above<FAR>(k.z, c, t.b_all));
         else if constexpr (F == kOwn)
             one_in += exp2_hw(above<FAR>(k.z, kLog2e, t.b_one));
-    }
+    });
     group_put<OpSum>(s_out, s.red[4]);
     group_put<OpSum>(s1, s.red[5]);
     group_put<OpSum>(s_in, s.red[6]);
@@ -222,10 +227,7 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, Row<TH> &R,
     // p log(p / q) - p + q for each outcome: what is added sums to 0 over all
     // outcomes, and a term is then small where p is near q
     float kl = 0.0f, qsum = 0.0f;
-#pragma unroll
-    for (int n = 0; n < R.NS; ++n) {
-        Slot &k = R.slot[n];
-        if (k.col < 0) continue;
+    R.slots([&](Slot &k, int n) {
         const float l = above<FAR>(k.z, c, t.b_all);
         k.p = expf(logp[n] - log_p);
         k.q = t.none ? 0.0f : exp2_hw(l) / t.s_all;
@@ -236,7 +238,7 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, Row<TH> &R,
         else
             kl += k.p * ((logp[n] - log_p) - (l * kLn2 - log_all)) - k.p + k.q;
         qsum += k.q;
-    }
+    });
     if (!a.loss) return t;
     group_put<OpSum>(kl, s.red[9]);
     group_put<OpSum>(qsum, s.red[10]);
@@ -308,22 +310,19 @@ __device__ __forceinline__ void rest_factors(const Stats &t, bool label, float c
 // The gradient at the slots and at the label, over what the sweep left there.
 // Synchronises first.
 template <int GT, bool FAR, LabelForm F, int TH>
-__device__ __forceinline__ void slot_gradient(const Row<TH> &R, const Stats &t, float f_out,
+__device__ __forceinline__ void slot_gradient(Row<TH> &R, const Stats &t, float f_out,
                                               float f_one, const uint32_t *bits,
                                               typename Elem<GT>::T *dz)
 {
     __syncthreads();
-#pragma unroll
-    for (int n = 0; n < R.NS; ++n) {
-        const Slot &k = R.slot[n];
-        if (k.col < 0) continue;
+    R.slots([&](const Slot &k, int) {
         float d = t.kd ? t.gk * (k.q - k.p) : 0.0f;
         if (R.y >= 0) {
             const float l = above_one<FAR, F>(k.z, R.c, t);
             d += t.ge * ((t.none ? 0.0f : exp2_hw(l) / t.s_one) - (k.col == R.y ? 1.0f : 0.0f));
         }
         dz[k.col] = narrow<GT>(d);
-    }
+    });
     if (threadIdx.x == 0 && R.y >= 0 && !is_marked(bits, R.y))
         dz[R.y] = narrow<GT>(rest_value<FAR, F>(R.zy, R.c, t, f_out, f_one) - t.ge);
 }

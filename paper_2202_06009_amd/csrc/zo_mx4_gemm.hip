@@ -38,81 +38,268 @@ __device__ __forceinline__ void unroll(F &&f)
     }
 }
 
-// Four consecutive results of a row, of which nv are inside it.
+// Two adjacent 16 x 16 tiles of results, u of columns n .. n + 15 and v of the next
+// 16: rows of 16 lanes swap halves so that a lane holds 8 consecutive columns (of
+// u in lanes 0..15 and 32..47, of v in the others) and a row of the output gets 64
+// (16-bit) or 128 bytes at once.
 template <int GT>
-__device__ __forceinline__ void store4(typename Elem<GT>::T *p, f32x4 v, int64_t nv)
+__device__ __forceinline__ void store_pair(typename Elem<GT>::T *row, int64_t n, int64_t cols,
+                                           bool inside, f32x4 u, f32x4 v, int lane)
 {
-    if (nv >= 4) {
-        if constexpr (GT == GT_F32) {
-            *reinterpret_cast<u32x4_a2 *>(p) = __builtin_bit_cast(u32x4, v);
-        } else {
-            const u32x2 w = {(uint32_t)narrow<GT>(v[0]) | (uint32_t)narrow<GT>(v[1]) << 16,
-                             (uint32_t)narrow<GT>(v[2]) | (uint32_t)narrow<GT>(v[3]) << 16};
-            *reinterpret_cast<u32x2_a2 *>(p) = w;
+    const int g = lane >> 4;
+    if constexpr (GT == GT_F32) {
+        // 16 bytes a lane as they are
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const f32x4 &x = h ? v : u;
+            const int64_t at = n + h * 16 + g * 4, nv = cols - at;
+            if (!inside) continue;
+            if (nv >= 4) {
+                *reinterpret_cast<u32x4_a2 *>(row + at) = __builtin_bit_cast(u32x4, x);
+            } else {
+                for (int q = 0; q < 4; ++q)
+                    if (q < nv) row[at + q] = __float_as_uint(x[q]);
+            }
         }
     } else {
+        u32x4 w;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (q < nv) p[q] = narrow<GT>(v[q]);
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t a = (uint32_t)narrow<GT>(u[2 * h]) |
+                               (uint32_t)narrow<GT>(u[2 * h + 1]) << 16;
+            const uint32_t b = (uint32_t)narrow<GT>(v[2 * h]) |
+                               (uint32_t)narrow<GT>(v[2 * h + 1]) << 16;
+            const auto s = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+            w[h] = s[0];
+            w[2 + h] = s[1];
+        }
+        const int64_t at = n + (g & 1) * 16 + (g >> 1) * 8, nv = cols - at;
+        if (!inside) return;
+        if (nv >= 8) {
+            *reinterpret_cast<u32x4_a2 *>(row + at) = w;
+        } else {
+            for (int q = 0; q < 8; ++q) {
+                if (q >= nv) break;
+                const uint32_t d = q < 2 ? w[0] : q < 4 ? w[1] : q < 6 ? w[2] : w[3];
+                row[at + q] = (uint16_t)(d >> (16 * (q & 1)));
+            }
+        }
     }
 }
 
-// 128 x 128 outputs per workgroup, 64 x 64 per wave, operands straight from
-// memory.
-template <int GT>
-__global__ __launch_bounds__(256) void k_mx4_product(Mx4View a, Mx4View b,
-                                                     typename Elem<GT>::T *__restrict__ out,
-                                                     int64_t ld, uint32_t n_tiles)
+// The workgroup's tile of the output.  Workgroups go to the 8 XCDs in turn, each
+// of which has an L2 of its own: an XCD gets a contiguous run of tiles, walked
+// down kBand rows of tiles at a time, so that its workgroups share operands.
+constexpr uint32_t kXcds = 8, kBand = 8;
+
+struct TileIndex {
+    uint32_t m, n;
+};
+
+__device__ __forceinline__ TileIndex tile_index(uint32_t wg, uint32_t m_tiles, uint32_t n_tiles)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t m0 = (int64_t)(blockIdx.x / n_tiles) * 128 + (wave >> 1) * 64;
-    const int64_t n0 = (int64_t)(blockIdx.x % n_tiles) * 128 + (wave & 1) * 64;
-    // a wave may lie wholly beyond the edge: the storage ends with its group of 64
-    if (m0 >= a.rows || n0 >= b.rows) return;
-    const uint8_t *pa = a.codes + m0 / 16 * a.kt * 1024 + lane * 16;
-    const uint8_t *pb = b.codes + n0 / 16 * b.kt * 1024 + lane * 16;
-    const uint8_t *sa = a.scales + m0 / 64 * a.kt * 256 + lane * 4;
-    const uint8_t *sb = b.scales + n0 / 64 * b.kt * 256 + lane * 4;
-    f32x4 acc[4][4] = {};
-    for (int64_t t = 0; t < a.kt; ++t) {
-        u32x4 x[4], w[4];
+    const uint32_t total = m_tiles * n_tiles;
+    const uint32_t each = total / kXcds, more = total % kXcds, x = wg % kXcds;
+    const uint32_t id = x * each + min(x, more) + wg / kXcds;
+    const uint32_t band = id / (kBand * n_tiles), in = id % (kBand * n_tiles);
+    const uint32_t height = min(kBand, m_tiles - band * kBand);
+    return {band * kBand + in % height, in / height};
+}
+
+// Where the 1 KiB tile of 16 rows x 128 columns with row tile index rt begins, at
+// column tile 0; row tiles beyond the matrix stand for the last that is stored
+// (what is computed from them is not stored).
+__device__ __forceinline__ const uint8_t *tile_at(const Mx4View &x, int64_t rt)
+{
+    const int64_t stored = (x.rows + 63) / 64 * 4;
+    return x.codes + min(rt, stored - 1) * x.kt * 1024;
+}
+
+// The same for the scales of 64 rows.
+__device__ __forceinline__ const uint8_t *scales_at(const Mx4View &x, int64_t group)
+{
+    const int64_t stored = (x.rows + 63) / 64;
+    return x.scales + min(group, stored - 1) * x.kt * 256;
+}
+
+// 32 MT x 16 WN NT outputs per workgroup of 2 x WN waves, 16 MT x 16 NT per wave, the
+// operands through shared memory in three buffers of one column tile each.
+//
+// A step multiplies one column tile.  Its first half (the wave's upper row tiles
+// of a) runs from fragments that are in registers while the lower half's are
+// read; then, past the step's one barrier, the second half runs while the next
+// step's first fragments are read from the next buffer (each of b's as soon as its
+// last product is under way), the tiles that were loaded two steps ago are written
+// to the buffer after that, and loads into their registers are issued: two steps
+// of loads are in flight, about what the memory's latency takes.
+// ODD: an odd number of steps (the register sets go round by twos).
+template <int GT, int MT, int NT, int WN, bool ODD>
+__global__ __launch_bounds__(128 * WN, 2) void k_mx4_product(
+    Mx4View a, Mx4View b, typename Elem<GT>::T *__restrict__ out, int64_t ld, uint32_t m_tiles,
+    uint32_t n_tiles)
+{
+    static_assert(MT / 2 <= NT, "a row tile's fragment is read per column tile");
+    static_assert(MT % 4 == 0 && NT % 4 == 0, "whole groups of 64 rows per wave");
+    constexpr int CHUNKS = 2 * MT + WN * NT, WAVES = 2 * WN;     // 1 KiB tiles of a step
+    constexpr int MINE = CHUNKS / WAVES;
+    constexpr int MS = MT / 4, NS = NT / 4, HALF = MT / 2;
+    extern __shared__ u32x4 lds[];                               // [3][CHUNKS][64]
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    const TileIndex tile = tile_index(blockIdx.x, m_tiles, n_tiles);
+    const int64_t m_tile = (int64_t)tile.m * 2 * MT;             // in tiles of 16
+    const int64_t n_tile = (int64_t)tile.n * WN * NT;
+    const int steps = (int)a.kt;
+
+    // this wave's share of the loads: chunk c < 2 MT is of a, the others of b
+    const uint8_t *src[MINE];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[i] = *reinterpret_cast<const u32x4 *>(pa + (i * a.kt + t) * 1024);
-            w[i] = *reinterpret_cast<const u32x4 *>(pb + (i * b.kt + t) * 1024);
-        }
-        const uint32_t ea = *reinterpret_cast<const uint32_t *>(sa + t * 256);
-        const uint32_t eb = *reinterpret_cast<const uint32_t *>(sb + t * 256);
-        unroll<4>([&](auto i) {
-            unroll<4>([&](auto j) {
-                acc[i][j] = mfma<decltype(j)::value, decltype(i)::value>(w[j], x[i], acc[i][j],
-                                                                         eb, ea);
-            });
+    for (int i = 0; i < MINE; ++i) {
+        const int c = i * WAVES + wave;
+        src[i] = c < 2 * MT ? tile_at(a, m_tile + c) : tile_at(b, n_tile + (c - 2 * MT));
+    }
+    const uint8_t *sa[MS], *sb[NS];
+#pragma unroll
+    for (int g = 0; g < MS; ++g) sa[g] = scales_at(a, m_tile / 4 + wm * MS + g);
+#pragma unroll
+    for (int g = 0; g < NS; ++g) sb[g] = scales_at(b, n_tile / 4 + wn * NS + g);
+
+    // set R holds the tiles and scales of the steps congruent to R modulo 2
+    u32x4 stage[2][MINE];
+    uint32_t ea[2][MS], eb[2][NS];
+    auto fetch = [&](auto set, int t) {
+        constexpr int R = decltype(set)::value;
+        const int64_t at = min(t, steps - 1);
+#pragma unroll
+        for (int i = 0; i < MINE; ++i)
+            stage[R][i] = *reinterpret_cast<const u32x4 *>(src[i] + at * 1024 + lane * 16);
+    };
+    auto read_scales = [&](auto set, int t) {
+        constexpr int R = decltype(set)::value;
+        const int64_t at = min(t, steps - 1);
+#pragma unroll
+        for (int g = 0; g < MS; ++g)
+            ea[R][g] = *reinterpret_cast<const uint32_t *>(sa[g] + at * 256 + lane * 4);
+#pragma unroll
+        for (int g = 0; g < NS; ++g)
+            eb[R][g] = *reinterpret_cast<const uint32_t *>(sb[g] + at * 256 + lane * 4);
+    };
+    auto put = [&](auto set, int buf) {
+        constexpr int R = decltype(set)::value;
+#pragma unroll
+        for (int i = 0; i < MINE; ++i)
+            lds[(buf * CHUNKS + i * WAVES + wave) * 64 + lane] = stage[R][i];
+    };
+    u32x4 fa[MT], fb[NT];
+    auto read_a = [&](int buf, auto i) {
+        constexpr int I = decltype(i)::value;
+        fa[I] = lds[(buf * CHUNKS + wm * MT + I) * 64 + lane];
+    };
+    auto read_b = [&](int buf, auto j) {
+        constexpr int J = decltype(j)::value;
+        fb[J] = lds[(buf * CHUNKS + 2 * MT + wn * NT + J) * 64 + lane];
+    };
+    f32x4 acc[MT][NT] = {};
+    // the products of half the row tiles with column tile j
+    auto multiply = [&](auto set, auto from, auto j) {
+        unroll<HALF>([&](auto i) {
+            constexpr int R = decltype(set)::value;
+            constexpr int I = decltype(from)::value + decltype(i)::value;
+            constexpr int J = decltype(j)::value;
+            acc[I][J] = mfma<J % 4, I % 4>(fb[J], fa[I], acc[I][J], eb[R][J / 4], ea[R][I / 4]);
         });
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t m = m0 + i * 16 + (lane & 15);
-        if (m >= a.rows) continue;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t n = n0 + j * 16 + (lane >> 4) * 4;
-            store4<GT>(out + m * ld + n, acc[i][j], b.rows - n);
+    };
+    using Zero = std::integral_constant<int, 0>;
+    using One = std::integral_constant<int, 1>;
+    using Lower = std::integral_constant<int, HALF>;
+    // step t, t congruent to `now` modulo 2, in buffer t modulo 3
+    int buf = 0;
+    auto step = [&](auto now, int t) {
+        const int next = buf == 2 ? 0 : buf + 1, after = next == 2 ? 0 : next + 1;
+        unroll<NT>([&](auto j) {
+            constexpr int J = decltype(j)::value;
+            if constexpr (J < HALF) read_a(buf, std::integral_constant<int, HALF + J>{});
+            multiply(now, Zero{}, j);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        __syncthreads();                        // every wave's tiles of step t + 1 are there
+        unroll<NT>([&](auto j) {
+            constexpr int J = decltype(j)::value;
+            if constexpr (J < HALF) read_a(next, j);
+            if constexpr (J == NT / 2 - 1) put(now, after);
+            if constexpr (J == NT / 2) fetch(now, t + 4);
+            multiply(now, Lower{}, j);
+            read_b(next, j);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        read_scales(now, t + 2);
+        buf = next;
+    };
+
+    if (steps > 0) {
+        fetch(Zero{}, 0);
+        fetch(One{}, 1);
+        read_scales(Zero{}, 0);
+        read_scales(One{}, 1);
+        put(Zero{}, 0);
+        fetch(Zero{}, 2);
+        put(One{}, 1);
+        fetch(One{}, 3);
+        __syncthreads();
+        unroll<NT>([&](auto j) { read_b(0, j); });
+        unroll<HALF>([&](auto i) { read_a(0, i); });
+        int t = 0;
+        for (; t + 1 < steps; t += 2) {
+            step(Zero{}, t);
+            step(One{}, t + 1);
         }
+        if constexpr (ODD) step(Zero{}, t);
     }
+
+    const int64_t m0 = m_tile * 16 + wm * MT * 16 + (lane & 15);
+    const int64_t n0 = n_tile * 16 + wn * NT * 16;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t m = m0 + i * 16;
+#pragma unroll
+        for (int j = 0; j < NT; j += 2)
+            store_pair<GT>(out + m * ld, n0 + j * 16, b.rows, m < a.rows, acc[i][j], acc[i][j + 1],
+                           lane);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+template <int GT, int MT, int NT, int WN>
+static hipError_t launch_tiles(const Mx4View &a, const Mx4View &b, void *out, int64_t ld,
+                               hipStream_t st)
+{
+    constexpr uint32_t lds = 3 * (2 * MT + WN * NT) * 1024;
+    const int64_t nt = (b.rows + 16 * WN * NT - 1) / (16 * WN * NT);
+    const int64_t mt = (a.rows + 32 * MT - 1) / (32 * MT), tiles = mt * nt;
+    if (tiles > INT32_MAX || a.kt > INT32_MAX) return hipErrorInvalidValue;
+    const auto kernel =
+        a.kt % 2 ? k_mx4_product<GT, MT, NT, WN, true> : k_mx4_product<GT, MT, NT, WN, false>;
+    if (lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(
+            reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+            (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    kernel<<<dim3((uint32_t)tiles), 128 * WN, lds, st>>>(
+        a, b, static_cast<typename Elem<GT>::T *>(out), ld, (uint32_t)mt, (uint32_t)nt);
+    return hipGetLastError();
 }
 
 hipError_t launch_mx4_product(const Mx4View &a, const Mx4View &b, void *out, int gt, int64_t ld,
                               hipStream_t st)
 {
     if (a.rows == 0 || b.rows == 0) return hipSuccess;
-    const int64_t nt = (b.rows + 127) / 128, tiles = (a.rows + 127) / 128 * nt;
-    if (tiles > INT32_MAX) return hipErrorInvalidValue;
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
-        k_mx4_product<GT><<<dim3((uint32_t)tiles), 256, 0, st>>>(
-            a, b, static_cast<typename Elem<GT>::T *>(out), ld, (uint32_t)nt);
-        return hipGetLastError();
+        const int64_t large = (a.rows + 255) / 256 * ((b.rows + 255) / 256);
+        if (large >= 128) return launch_tiles<GT, 8, 4, 4>(a, b, out, ld, st);
+        return launch_tiles<GT, 4, 4, 2>(a, b, out, ld, st);
     });
 }
 
