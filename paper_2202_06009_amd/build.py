@@ -17,10 +17,11 @@ SOURCES = [os.path.join(CSRC, f) for f in ("zo_kernels.hip", "zo_server.hip",
                                            "zo_server_many.hip", "zo_server_ua.hip",
                                            "zo_kernels_ua.hip", "zo_adam.cpp",
                                            "zo_mx4_quant.hip", "zo_mx4_gemm.hip",
+                                           "zo_mx4_few.hip",
                                            "zo_top.hip", "zo_distill.hip", "zo_ops.cpp")]
 HEADERS = [os.path.join(ROOT, "include", "zo_adam.h"), os.path.join(ROOT, "include", "zo_ops.h"),
            os.path.join(CSRC, "zo_internal.h"), os.path.join(CSRC, "zo_ops_internal.h"),
-           os.path.join(CSRC, "zo_ops_device.h"),
+           os.path.join(CSRC, "zo_ops_device.h"), os.path.join(CSRC, "zo_mx4_device.h"),
            os.path.join(CSRC, "zo_device.h"), os.path.join(CSRC, "zo_server.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-ffp-contract=off", "-fno-fast-math",

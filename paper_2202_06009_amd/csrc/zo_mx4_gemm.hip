@@ -10,23 +10,9 @@
 //
 // With b's rows as the first operand, lane l's four results are columns
 // n = 4 (l / 16) .. + 3 of row m = l % 16 of the output.
-#include "zo_ops_device.h"
+#include "zo_mx4_device.h"
 
 namespace zo {
-
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-// acc += a-tile x b-tile; SA / SB: which byte of the scale dwords.
-template <int SA, int SB>
-__device__ __forceinline__ f32x4 mfma(const u32x4 &a, const u32x4 &b, f32x4 acc, uint32_t sa,
-                                      uint32_t sb)
-{
-    const i32x8 x = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
-    const i32x8 y = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 4, 4, SA, (int)sa, SB,
-                                                            (int)sb);
-}
 
 // Calls f(integral_constant<0>) .. f(integral_constant<N - 1>).
 template <int N, class F>
@@ -295,11 +281,15 @@ hipError_t launch_mx4_product(const Mx4View &a, const Mx4View &b, void *out, int
                               hipStream_t st)
 {
     if (a.rows == 0 || b.rows == 0) return hipSuccess;
+    if (a.rows <= kFewRows) return launch_mx4_few(a, b, out, gt, ld, st);
+    const auto count = [&](int64_t m, int64_t n) {
+        return (a.rows + m - 1) / m * ((b.rows + n - 1) / n);
+    };
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
-        const int64_t large = (a.rows + 255) / 256 * ((b.rows + 255) / 256);
-        if (large >= 128) return launch_tiles<GT, 8, 4, 4>(a, b, out, ld, st);
-        return launch_tiles<GT, 4, 4, 2>(a, b, out, ld, st);
+        if (count(256, 256) >= 224) return launch_tiles<GT, 8, 4, 4>(a, b, out, ld, st);
+        if (count(128, 128) >= 144) return launch_tiles<GT, 4, 4, 2>(a, b, out, ld, st);
+        return launch_tiles<GT, 4, 4, 1>(a, b, out, ld, st);
     });
 }
 

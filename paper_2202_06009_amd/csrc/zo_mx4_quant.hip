@@ -13,51 +13,9 @@
 // row's 128 elements, 8 each, so that four lanes hold a block, and the four
 // 16-row passes of a 64-row group make up the dwords in which the scales are
 // stored.  For the column form the tile goes through shared memory once.
-#include "zo_ops_device.h"
+#include "zo_mx4_device.h"
 
 namespace zo {
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-
-// Largest magnitude bits of the 8 elements of a lane (dwords of one element in
-// binary32, of two otherwise, then the larger of the two).
-template <int GT>
-__device__ __forceinline__ uint32_t mag(uint32_t a, uint32_t w)
-{
-    if constexpr (GT == GT_F32) {
-        return max(a, w & 0x7FFFFFFFu);
-    } else {
-        return __builtin_bit_cast(
-            uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
-                                                __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu)));
-    }
-}
-
-// Scale byte of a block from its largest magnitude's bits.
-template <int GT>
-__device__ __forceinline__ uint32_t scale_byte(uint32_t a)
-{
-    const uint32_t e = __float_as_uint(widen<GT>((typename Elem<GT>::T)a)) >> 23;
-    return e == 255 ? 255u : (uint32_t)max((int)e - 2, 0);
-}
-
-// Two elements (dwords w0 and w1 in binary32, the halves of w0 otherwise) into
-// byte B of `old`.
-template <int GT, int B>
-__device__ __forceinline__ uint32_t convert2(uint32_t old, uint32_t w0, uint32_t w1, float scale)
-{
-    if constexpr (GT == GT_F32)
-        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(old, __uint_as_float(w0),
-                                                        __uint_as_float(w1), scale, B);
-    else if constexpr (GT == GT_BF16)
-        return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, __builtin_bit_cast(bf16x2, w0),
-                                                         scale, B);
-    else
-        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(old, __builtin_bit_cast(f16x2, w0),
-                                                        scale, B);
-}
 
 template <int GT>
 constexpr int kTileRows = GT == GT_F32 ? 64 : 128;

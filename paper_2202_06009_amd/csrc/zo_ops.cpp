@@ -138,6 +138,9 @@ int zo_mx4_linear(const void *x, int32_t dtype, int64_t ldx, const zo_mx4 *w, co
     if (!fits_a_launch(xq->rows, w->rows) || !fits_a_launch(xq->rows, xq->cols))
         return ZO_EINVAL;
     const zo::Mx4View v = view(xq);
+    if (v.rows && w->rows && zo::few_fused(v.rows, v.cols))
+        return from_hip(zo::launch_mx4_few_fused(x, gx, v.rows, v.cols, ldx, view(w), out, go, ldo,
+                                                 stream));
     rc = from_hip(zo::launch_mx4_quantize(x, gx, xq->rows, xq->cols, ldx, &v, nullptr, stream));
     if (rc) return rc;
     return from_hip(zo::launch_mx4_product(v, view(w), out, go, ldo, stream));
