@@ -14,9 +14,10 @@ import ctypes
 
 import torch
 
-from . import ZoError, ZO_EHIP, ZO_OK, _Distill, _Mx4, lib
+from . import ZoError, ZO_EHIP, ZO_EINVAL, ZO_OK, _Distill, _Mx4, lib
 
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_MAX_DIM = 1 << 30
 
 
 def _size(n, where):
@@ -50,22 +51,28 @@ class Mx4:
     ``scales``, uint8 device tensors in the layout of ``zo_mx4`` (allocated when
     not given).  Its rows are the axis that products reduce over."""
 
-    __slots__ = ("rows", "cols", "codes", "scales", "_c")
+    __slots__ = ("rows", "cols", "codes", "scales", "dev", "_c", "_at")
 
     def __init__(self, rows, cols, codes=None, scales=None, device="cuda"):
-        self.rows, self.cols = int(rows), int(cols)
-        nc, ns = zo_mx4_code_bytes(rows, cols), zo_mx4_scale_bytes(rows, cols)
+        rows, cols = int(rows), int(cols)
+        if not (0 <= rows <= _MAX_DIM and 0 <= cols <= _MAX_DIM):
+            raise ZoError(ZO_EINVAL, "Mx4")
+        tiles = ((rows + 63) >> 6) * ((cols + 127) >> 7)     # of 64 rows x 128 columns
         if codes is None:
-            codes = torch.empty(nc, dtype=torch.uint8, device=device)
+            codes = torch.empty(tiles * 4096, dtype=torch.uint8, device=device)
         if scales is None:
-            scales = torch.empty(ns, dtype=torch.uint8, device=codes.device)
-        for t, n, what in ((codes, nc, "codes"), (scales, ns, "scales")):
-            if t.dtype != torch.uint8:
+            scales = torch.empty(tiles * 256, dtype=torch.uint8, device=codes.device)
+        for t, n, what in ((codes, tiles * 4096, "codes"), (scales, tiles * 256, "scales")):
+            if t.dtype is not torch.uint8:
                 raise ValueError(f"{what}: expected uint8, got {t.dtype}")
-            if not t.is_contiguous() or t.numel() < n:
+            if t.numel() < n or not t.is_contiguous():
                 raise ValueError(f"{what}: needs {n} contiguous elements, has {t.numel()}")
-        self.codes, self.scales = codes, scales
-        self._c = _Mx4(codes.data_ptr(), scales.data_ptr(), self.rows, self.cols)
+        dev = codes.get_device()
+        if dev < 0 or scales.get_device() != dev:
+            raise ValueError("codes, scales: expected tensors on one GPU")
+        self.rows, self.cols, self.codes, self.scales, self.dev = rows, cols, codes, scales, dev
+        self._c = _Mx4(codes.data_ptr(), scales.data_ptr(), rows, cols)
+        self._at = ctypes.addressof(self._c)
 
 
 # The checks below read each attribute of a tensor once: a decode step calls
@@ -85,21 +92,23 @@ def _device_of(t, what):
     return dev
 
 
-def _matrix(t, what, dev, shape=None):
-    """(pointer, element type, row stride) of a matrix with contiguous rows."""
+def _matrix(t, what, dev, rows=None, cols=None):
+    """(pointer, element type, row stride) of a matrix with contiguous rows, of
+    rows x cols when given."""
     code = _DTYPES.get(t.dtype)
     if code is None:
         raise ValueError(f"{what}: expected float32, float16 or bfloat16, got {t.dtype}")
-    have = t.shape
-    if len(have) != 2 or (shape is not None and tuple(have) != shape):
-        raise ValueError(f"{what}: expected shape {shape or '2-d'}, got {tuple(have)}")
-    rows, cols = have
+    if t.dim() != 2:
+        raise ValueError(f"{what}: expected a matrix, got shape {tuple(t.shape)}")
+    r, c = t.shape
+    if rows is not None and (r != rows or c != cols):
+        raise ValueError(f"{what}: expected shape {(rows, cols)}, got {(r, c)}")
     ld, step = t.stride()
-    if step != 1 and cols > 1:
+    if step != 1 and c > 1:
         raise ValueError(f"{what}: expected contiguous rows")
-    if rows <= 1 or cols == 0:
-        ld = max(cols, 1)
-    elif ld < cols:
+    if r <= 1 or c == 0:
+        ld = c or 1
+    elif ld < c:
         raise ValueError(f"{what}: rows overlap")
     return _at(t, what, dev), code, ld
 
@@ -107,20 +116,20 @@ def _matrix(t, what, dev, shape=None):
 def _vector(t, what, dev, dtype, shape):
     if t is None:
         return None
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
-    if tuple(t.shape) != shape or not t.is_contiguous():
+    if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what}: expected contiguous {shape}, got {tuple(t.shape)}")
     return _at(t, what, dev)
 
 
 def _mx4(q, what, dev):
     """Address of q's C struct."""
-    if not isinstance(q, Mx4):
+    if type(q) is not Mx4:
         raise ValueError(f"{what}: expected an Mx4")
-    if q.codes.get_device() != dev or q.scales.get_device() != dev:
-        raise ValueError(f"{what}: expected an Mx4 on GPU {dev}")
-    return ctypes.addressof(q._c)
+    if q.dev != dev:
+        raise ValueError(f"{what}: expected an Mx4 on GPU {dev}, got one on GPU {q.dev}")
+    return q._at
 
 
 def _workspace(ws, nbytes, dev, stream):
@@ -136,23 +145,27 @@ def _workspace(ws, nbytes, dev, stream):
     return ws
 
 
+_functions = {}
+
+
 def _run(where, dev, stream, args, tensors):
     """Calls the C function on `stream` (the current stream of GPU `dev` when None);
     `tensors` are those that the kernels touch."""
-    f = getattr(lib(), where)
+    f = _functions.get(where)
+    if f is None:
+        f = _functions[where] = getattr(lib(), where)
     if dev != torch.cuda.current_device():
         with torch.cuda.device(dev):
             return _run(where, dev, stream, args, tensors)
     current = torch._C._cuda_getCurrentRawStream(dev)
-    s = current if stream is None else stream.cuda_stream
-    rc = f(*args, s)
-    if s != current:
+    if stream is None or stream.cuda_stream == current:
+        rc = f(*args, current)
+    else:
+        rc = f(*args, stream.cuda_stream)
         for t in tensors:
-            if isinstance(t, Mx4):
-                t.codes.record_stream(stream)
-                t.scales.record_stream(stream)
-            elif t is not None:
-                t.record_stream(stream)
+            for x in ((t.codes, t.scales) if type(t) is Mx4 else (t,)):
+                if x is not None:
+                    x.record_stream(stream)
     if rc != ZO_OK:
         detail = lib().zo_ops_last_hip_error().decode() if rc == ZO_EHIP else ""
         raise ZoError(rc, where, detail)
@@ -173,7 +186,7 @@ def zo_mx4_dequantize(q, out, stream=None):
     """The values of q into out [q.rows, q.cols]."""
     dev = _device_of(out, "out")
     pq = _mx4(q, "q", dev)
-    p, dt, ld = _matrix(out, "out", dev, (q.rows, q.cols))
+    p, dt, ld = _matrix(out, "out", dev, q.rows, q.cols)
     _run("zo_mx4_dequantize", dev, stream, (pq, p, dt, ld), (q, out))
 
 
@@ -181,7 +194,7 @@ def zo_mx4_product(a, b, out, stream=None):
     """out [a.rows, b.rows] = a b^T, reduced over the columns of both."""
     dev = _device_of(out, "out")
     pa, pb = _mx4(a, "a", dev), _mx4(b, "b", dev)
-    p, dt, ld = _matrix(out, "out", dev, (a.rows, b.rows))
+    p, dt, ld = _matrix(out, "out", dev, a.rows, b.rows)
     _run("zo_mx4_product", dev, stream, (pa, pb, p, dt, ld), (a, b, out))
 
 
@@ -190,8 +203,8 @@ def zo_mx4_linear(x, w, out, xq, stream=None):
     x's shape) is workspace."""
     dev = _device_of(x, "x")
     pw, pq = _mx4(w, "w", dev), _mx4(xq, "xq", dev)
-    px, dx, ldx = _matrix(x, "x", dev, (xq.rows, xq.cols))
-    po, do, ldo = _matrix(out, "out", dev, (xq.rows, w.rows))
+    px, dx, ldx = _matrix(x, "x", dev, xq.rows, xq.cols)
+    po, do, ldo = _matrix(out, "out", dev, xq.rows, w.rows)
     _run("zo_mx4_linear", dev, stream, (px, dx, ldx, pw, pq, po, do, ldo), (x, w, out, xq))
 
 
@@ -237,7 +250,7 @@ def zo_distill_loss(z, values, columns, loss=None, dz=None, *, tau=1.0, teacher_
     if dz is not None:
         if dz.dtype != z.dtype:
             raise ValueError(f"dz: expected {z.dtype}, got {dz.dtype}")
-        pdz, _, lddz = _matrix(dz, "dz", dev, (rows, vocab))
+        pdz, _, lddz = _matrix(dz, "dz", dev, rows, vocab)
     ws = _workspace(ws, zo_distill_ws(rows, vocab), dev, stream)
     pw, nw = (None, 0) if ws is None else (ws.data_ptr(), ws.numel())
     a = _Distill(p, dt, rows, vocab, ldz, top,
