@@ -12,9 +12,10 @@
 // order above the complement of the column, so that of equal logits the lowest
 // column comes first and no order of the collection shows.
 //
-// Rows on which this collects more than it has room for (ties, masks), rows
-// with NaN, and rows that do not fit are counted digit by digit from memory
-// (select_row): exact for everything, several reads.
+// Rows that do not fit are read twice (k_top_long).  Rows on which this collects
+// more than it has room for (ties, masks) and rows with NaN or +infinity are
+// counted digit by digit from memory (select_row): exact for everything, several
+// reads.
 #include "zo_ops_device.h"
 
 namespace zo {
@@ -215,18 +216,148 @@ __device__ void lse_row(const TopArgs &a, int64_t row, TopShared<TH> &s)
                             group_get<OpMax, TH / 64>(s.red[1]) > 0.0f);
 }
 
-// Rows that do not fit registers.
-template <int GT>
-__global__ __launch_bounds__(1024) void k_top_long(TopArgs a)
-{
-    __shared__ TopShared<1024> s;
-    if (a.lse) lse_row<GT, 1024>(a, blockIdx.x, s);
-    select_row<GT, 1024>(a, blockIdx.x, s);
-}
-
 // Groups of the vectors of a thread, when more than a quarter as many logits are
 // wanted as there are threads.
 constexpr int kGroups = 4;
+
+// A thread's part in the bound: its largest logit, those of its groups, and which
+// of the groups have logits (bit g).
+struct GroupMaxima {
+    float all, of[kGroups];
+    uint32_t there;
+};
+
+// The key of a lower bound of the `top`-th largest logit from the group maxima, the
+// largest of which is M.  s.hist is zero.  Synchronises.
+template <int TH>
+__device__ __forceinline__ uint32_t find_bound(TopShared<TH> &s, uint32_t top, float M,
+                                               const GroupMaxima &m)
+{
+    constexpr int NW = TH / 64;
+    const int tid = threadIdx.x;
+    const bool by_thread = top <= TH / kGroups;
+    float lo = INFINITY;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+        if (m.there >> g & 1) lo = fminf(lo, m.of[g]);
+    if (by_thread) lo = m.there ? m.all : INFINITY;
+    group_put<OpMin>(lo, s.red[1]);
+    __syncthreads();
+    lo = group_get<OpMin, NW>(s.red[1]);
+    // bins of key - key(lo), shifted until 256 cover the range; a NaN falls in none
+    const uint32_t klo = order_key(lo);
+    const int shift = max(0, 24 - __clz((int)(order_key(M) - klo)));
+    const int fine = max(0, shift - 8);
+    auto count = [&](uint32_t from, int by, uint32_t bins) {
+        auto one = [&](float g, bool there) {
+            const uint32_t k = (order_key(g) - from) >> by;
+            if (there && k < bins) atomicAdd(&s.hist[k], 1u);
+        };
+        if (by_thread) {
+            one(m.all, m.there != 0);
+        } else {
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) one(m.of[g], m.there >> g & 1);
+        }
+    };
+    count(klo, shift, 256);
+    __syncthreads();
+    find_bin<TH>(s, top);
+    __syncthreads();
+    const uint32_t left = s.sel[1];
+    uint32_t least = klo + (s.sel[0] << shift);
+    if (shift > 0 && s.sel[2] > top + 64) {
+        __syncthreads();
+        for (int i = tid; i < 256; i += TH) s.hist[i] = 0;
+        __syncthreads();
+        count(least, fine, 1u << (shift - fine));
+        __syncthreads();
+        find_bin<TH>(s, left);
+        __syncthreads();
+        least += s.sel[0] << fine;
+    }
+    return least;
+}
+
+// A logit that reaches the bound joins the candidates, while there is room.
+template <int TH>
+__device__ __forceinline__ void offer(TopShared<TH> &s, float v, int64_t i)
+{
+    const uint32_t at = atomicAdd(&s.sel[3], 1u);
+    if (at < kRoom) s.cand[at] = full_key(order_key(v), (uint32_t)i);
+}
+
+// Rows that do not fit registers: the same with a second read of the row, the sums
+// from the differences (as lse_row).
+template <int GT>
+__global__ __launch_bounds__(1024) void k_top_long(TopArgs a)
+{
+    constexpr int TH = 1024, NW = TH / 64, K = Elem<GT>::kVec;
+    __shared__ TopShared<TH> s;
+    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x, V = a.vocab;
+    const auto *z = static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ld;
+    const float c = kLog2e / a.tau;
+    for (int i = tid; i < 256; i += TH) s.hist[i] = 0;
+    if (tid == 0) s.sel[3] = 0;
+    GroupMaxima m = {-INFINITY, {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, 0};
+    float sum = 0.0f;
+    for (int64_t i0 = (int64_t)tid * K; i0 < V; i0 += kGroups * TH * K) {
+        u32x4 w[kGroups];
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const int64_t i = i0 + g * TH * K;
+            w[g] = load16<GT>(z + i, V - i, kNegInf<GT> & kElemMask<GT>);
+            if (i < V) m.there |= 1u << g;
+        }
+        float top = m.all;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const float v = max_of<GT>(w[g]);
+            m.of[g] = fmaxf(m.of[g], v);
+            top = fmaxf(top, v);
+        }
+        if (top != m.all) {
+            sum *= m.all == -INFINITY ? 0.0f : exp2_hw((m.all - top) * c);
+            m.all = top;
+        }
+        const float b = m.all == -INFINITY ? 0.0f : m.all;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+            for (int q = 0; q < K; ++q) sum += exp2_hw((elem_of<GT>(w[g], q) - b) * c);
+    }
+    group_put<OpMax>(m.all, s.red[0]);
+    __syncthreads();
+    const float M = group_get<OpMax, NW>(s.red[0]);
+    if (m.all != -INFINITY) sum *= exp2_hw((m.all - M) * c);
+    group_put<OpSum>(sum, s.red[2]);
+    const uint32_t least = find_bound<TH>(s, (uint32_t)a.top, M, m);
+    const float total = group_get<OpSum, NW>(s.red[2]);
+    if (total != total) {                                // NaN or an infinity is about
+        if (a.lse) lse_row<GT, TH>(a, row, s);
+        select_row<GT, TH>(a, row, s);
+        return;
+    }
+    if (a.lse && tid == 0) a.lse[row] = lse_of(M, total, a.tau, false);
+    const float bound = key_value(least);
+    for (int64_t i = (int64_t)tid * K; i < V; i += TH * K) {
+        const u32x4 w = load16<GT>(z + i, V - i, kNegInf<GT> & kElemMask<GT>);
+        if (max_of<GT>(w) >= bound) {
+#pragma unroll
+            for (int q = 0; q < K; ++q) {
+                const float v = elem_of<GT>(w, q);
+                if (v >= bound && i + q < V) offer<TH>(s, v, i + q);
+            }
+        }
+    }
+    __syncthreads();
+    const uint32_t n = s.sel[3];
+    if (n > kRoom)
+        select_row<GT, TH>(a, row, s);
+    else
+        sort_out<TH>(a, row, s, (int)n);
+}
 
 template <int GT, int TH, int NV>
 __global__ __launch_bounds__(TH, 4) void k_top(TopArgs a)
@@ -240,30 +371,21 @@ __global__ __launch_bounds__(TH, 4) void k_top(TopArgs a)
     for (int i = tid; i < 256; i += TH) s.hist[i] = 0;
     if (tid == 0) s.sel[3] = 0;
 
-    // groups: the threads that have logits, or kGroups of every thread's vectors
-    const bool by_thread = a.top <= TH / kGroups;
-    const bool mine = tid < x.vecs || x.has_last(V);
-    float m = x.last, lo = INFINITY, gm[kGroups];
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) gm[g] = -INFINITY;
+    GroupMaxima m = {x.last, {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, 0};
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        if (v * TH < x.vecs) {                           // the same for all threads
-            gm[v % kGroups] = fmaxf(gm[v % kGroups], max_of<GT>(x.w[v]));
-        }
+        if (v * TH < x.vecs)                             // the same for all threads
+            m.of[v % kGroups] = fmaxf(m.of[v % kGroups], max_of<GT>(x.w[v]));
         __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
-        m = fmaxf(m, gm[g]);
-        if (x.at(g) < x.vecs) lo = fminf(lo, gm[g]);
+        m.all = fmaxf(m.all, m.of[g]);
+        if (x.at(g) < x.vecs) m.there |= 1u << g;
     }
-    if (by_thread) lo = mine ? m : INFINITY;
-    group_put<OpMax>(m, s.red[0]);
-    group_put<OpMin>(lo, s.red[1]);
+    group_put<OpMax>(m.all, s.red[0]);
     __syncthreads();
     const float M = group_get<OpMax, NW>(s.red[0]);
-    lo = group_get<OpMin, NW>(s.red[1]);
 
     // sum of 2^(c z - r); its NaN also tells of a row with NaN or +infinity (the
     // maxima pass over NaN)
@@ -280,47 +402,17 @@ __global__ __launch_bounds__(TH, 4) void k_top(TopArgs a)
     }
     group_put<OpSum>(sum, s.red[2]);
 
-    // bins of the group maxima: key - key(lo), shifted until 256 bins cover them
-    const bool all = V <= kRoom;                         // every logit is a candidate
-    uint32_t least = 0;                                  // key of the lowest candidate
-    if (!all) {
-        const uint32_t klo = order_key(lo);
-        const int shift = max(0, 24 - __clz((int)(order_key(M) - klo)));
-        const int fine = max(0, shift - 8);
-        auto count = [&](float g, bool there, uint32_t from, int by, uint32_t bins) {
-            const uint32_t k = (order_key(g) - from) >> by;
-            if (there && k < bins) atomicAdd(&s.hist[k], 1u);
-        };
-        auto count_all = [&](uint32_t from, int by, uint32_t bins) {
-            if (by_thread) {
-                count(m, mine, from, by, bins);
-            } else {
-#pragma unroll
-                for (int g = 0; g < kGroups; ++g)
-                    count(gm[g], x.at(g) < x.vecs, from, by, bins);
-            }
-        };
-        count_all(klo, shift, 256);
+    // where the groups are not several times as many as are wanted, every logit of a
+    // short row is a candidate; fewer groups than wanted logits bound nothing
+    const int groups = min(x.vecs, a.top <= TH / kGroups ? TH : TH * kGroups);
+    const bool all = 2 * a.top > groups && V <= kRoom, unbound = !all && groups < a.top;
+    uint32_t least = 0;
+    if (all || unbound)
         __syncthreads();
-        find_bin<TH>(s, (uint32_t)a.top);
-        __syncthreads();
-        const uint32_t left = s.sel[1];
-        least = klo + (s.sel[0] << shift);
-        if (shift > 0 && s.sel[2] > (uint32_t)a.top + 64) {
-            __syncthreads();
-            for (int i = tid; i < 256; i += TH) s.hist[i] = 0;
-            __syncthreads();
-            count_all(least, fine, 1u << (shift - fine));
-            __syncthreads();
-            find_bin<TH>(s, left);
-            __syncthreads();
-            least += s.sel[0] << fine;
-        }
-    } else {
-        __syncthreads();
-    }
+    else
+        least = find_bound<TH>(s, (uint32_t)a.top, M, m);
     const float total = group_get<OpSum, NW>(s.red[2]);
-    if (total != total || !(fabsf(r) < 0x1p126f)) {      // or c z near overflow
+    if (total != total || !(fabsf(r) < 0x1p126f) || unbound) {   // or c z near overflow
         if (a.lse) lse_row<GT, TH>(a, row, s);
         select_row<GT, TH>(a, row, s);
         return;
@@ -328,19 +420,16 @@ __global__ __launch_bounds__(TH, 4) void k_top(TopArgs a)
     if (a.lse && tid == 0) a.lse[row] = lse_of(M, total, a.tau, false);
     // collect
     const float bound = key_value(least);
-    auto offer = [&](float z, int i) {
-        if (all || z >= bound) {
-            const uint32_t at = atomicAdd(&s.sel[3], 1u);
-            if (at < kRoom) s.cand[at] = full_key(order_key(z), (uint32_t)i);
-        }
-    };
-    if (x.has_last(V)) offer(x.last, x.last_column());
+    if (x.has_last(V) && (all || x.last >= bound)) offer<TH>(s, x.last, x.last_column());
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         repack<GT>(x.w[v]);
         if (x.at(v) < x.vecs && (all || max_of<GT>(x.w[v]) >= bound)) {
 #pragma unroll
-            for (int q = 0; q < K; ++q) offer(elem_of<GT>(x.w[v], q), x.at(v) * K + q);
+            for (int q = 0; q < K; ++q) {
+                const float z = elem_of<GT>(x.w[v], q);
+                if (all || z >= bound) offer<TH>(s, z, x.at(v) * K + q);
+            }
         }
         __builtin_amdgcn_sched_barrier(0);
     }
@@ -366,9 +455,7 @@ hipError_t launch_top_logits(const TopArgs &a, int gt, hipStream_t st)
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
         const int64_t vecs = a.vocab / Elem<GT>::kVec;
-        // few: fewer groups with logits than are wanted bound nothing
-        const bool few = a.vocab > kRoom && a.top > 64 && a.top > vecs;
-        if (few || vecs > 1024 * 16) {
+        if (vecs > 1024 * 16) {
             k_top_long<GT><<<dim3((uint32_t)a.rows), 1024, 0, st>>>(a);
             return hipGetLastError();
         }
