@@ -53,36 +53,32 @@ __device__ __forceinline__ float between(float b, float to, float c)
 // given), as e^2, by an exponential of its own.
 enum LabelForm { kSame, kSquare, kOwn };
 
-// A slot of the teacher: its column (-1: unused), the two logits, and, once the
-// row's statistics are known, the two probabilities.
-struct Slot {
-    int32_t col;
-    float u, z, p, q;
-};
-
+// The teacher's slots of a row: their columns (-1: unused), the two logits, and,
+// once the row's statistics are known, the two probabilities.  In shared memory:
+// the registers hold the row.  Slot j belongs to thread j modulo TH.
 template <int TH>
 struct DistillShared {
     int32_t col[kMaxTop];
+    float u[kMaxTop], z[kMaxTop], p[kMaxTop], q[kMaxTop];
     float red[12][TH / 64];
     int dup;
 };
 
 template <int TH>
 struct Row {
-    static constexpr int NS = kMaxTop / TH, NW = TH / 64;
+    static constexpr int NW = TH / 64;
     int64_t row, V;
     float w, c;              // weight, log2(e) / tau
     int32_t y;               // label, or -1
     float zy;
     bool tail;
-    Slot slot[NS];
-    // Calls f(slot) for the thread's used slots; waves without one skip it.
+    int top;
+    // Calls f(j) for the thread's used slots.
     template <class F>
-    __device__ __forceinline__ void slots(F &&f)
+    __device__ __forceinline__ void slots(const DistillShared<TH> &s, F &&f) const
     {
-#pragma unroll
-        for (int n = 0; n < NS; ++n)
-            if (__ballot(slot[n].col >= 0) != 0 && slot[n].col >= 0) f(slot[n], n);
+        for (int j = threadIdx.x; j < top; j += TH)
+            if (s.col[j] >= 0) f(j);
     }
 };
 
@@ -125,6 +121,7 @@ __device__ __forceinline__ bool read_row(const zo_distill &a, Row<TH> &R, Distil
     const int tid = threadIdx.x;
     R.row = blockIdx.x;
     R.V = a.vocab;
+    R.top = a.top;
     R.c = kLog2e / a.tau;
     R.tail = a.teacher_lse != nullptr;
     R.w = a.row_weight ? a.row_weight[R.row] : 1.0f;
@@ -134,34 +131,32 @@ __device__ __forceinline__ bool read_row(const zo_distill &a, Row<TH> &R, Distil
     R.zy = R.y >= 0 ? widen<GT>(z[R.y]) : 0.0f;
     for (int i = tid; i < (int)((R.V + 31) / 32); i += TH) bits[i] = 0;
     if (tid == 0) s.dup = 0;
-#pragma unroll
-    for (int n = 0; n < R.NS; ++n) {
-        const int j = n * TH + tid;
-        Slot t = {-1, -INFINITY, -INFINITY, 0.0f, 0.0f};
-        if (j < a.top) {
-            const int32_t col = a.columns[R.row * a.top + j];
-            if (col >= 0 && col < R.V)
-                t = {col, a.values[R.row * a.top + j], widen<GT>(z[col]), 0.0f, 0.0f};
-            s.col[j] = t.col;
-        }
-        R.slot[n] = t;
+    for (int j = tid; j < a.top; j += TH) {
+        const int32_t col = a.columns[R.row * a.top + j];
+        const bool used = col >= 0 && col < R.V;
+        s.col[j] = used ? col : -1;
+        s.u[j] = used ? a.values[R.row * a.top + j] : -INFINITY;
+        s.z[j] = used ? widen<GT>(z[col]) : -INFINITY;
     }
     __syncthreads();
-#pragma unroll
-    for (int n = 0; n < R.NS; ++n) {
-        const int32_t col = R.slot[n].col;
-        if (col >= 0 && (atomicOr(&bits[col >> 5], 1u << (col & 31)) >> (col & 31) & 1))
-            s.dup = 1;
-    }
+    R.slots(s, [&](int j) {
+        const int32_t col = s.col[j];
+        if (atomicOr(&bits[col >> 5], 1u << (col & 31)) >> (col & 31) & 1) s.dup = 1;
+    });
     __syncthreads();
     if (s.dup) {                        // of equal columns the first counts
-#pragma unroll
-        for (int n = 0; n < R.NS; ++n) {
+        // judged from the columns as they were, noted in p, then applied
+        for (int j = tid; j < a.top; j += TH) {
             bool again = false;
-            if (R.slot[n].col >= 0)
-                for (int i = 0; i < n * TH + tid; ++i) again |= s.col[i] == R.slot[n].col;
-            if (again) R.slot[n] = {-1, -INFINITY, -INFINITY, 0.0f, 0.0f};
+            for (int i = 0; i < j; ++i) again |= s.col[i] == s.col[j];
+            s.p[j] = again ? 1.0f : 0.0f;
         }
+        __syncthreads();
+        for (int j = tid; j < a.top; j += TH)
+            if (s.p[j] != 0.0f) {
+                s.col[j] = -1;
+                s.u[j] = s.z[j] = -INFINITY;
+            }
     }
     return true;
 }
@@ -170,7 +165,7 @@ __device__ __forceinline__ bool read_row(const zo_distill &a, Row<TH> &R, Distil
 // unless it follows from e) with the slots; writes the loss.  m_in: the slots'
 // largest logit, um the largest teacher's.  Synchronises.
 template <bool FAR, LabelForm F, int TH>
-__device__ __forceinline__ Stats statistics(const zo_distill &a, Row<TH> &R,
+__device__ __forceinline__ Stats statistics(const zo_distill &a, const Row<TH> &R,
                                             DistillShared<TH> &s, float m_out, float m_in,
                                             float um, float s_out, float s1)
 {
@@ -184,16 +179,18 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, Row<TH> &R,
     t.ge = R.w * a.ce_weight;
     t.kd = a.kd_weight != 0.0f && (R.tail || um != -INFINITY);
     const float lse = R.tail ? a.teacher_lse[R.row] : 0.0f, u0 = R.tail ? 0.0f : um;
-    float logp[Row<TH>::NS], s_in = 0.0f, one_in = 0.0f, psum = 0.0f;
-    R.slots([&](Slot &k, int n) {
-        logp[n] = -INFINITY;
-        if (k.u != -INFINITY) logp[n] = (k.u - u0) / a.tau - lse;
-        psum += expf(logp[n]);
-        s_in += exp2_hw(above<FAR>(k.z, c, t.b_all));
+    // log p up to the sum of p, kept in s.p
+    float s_in = 0.0f, one_in = 0.0f, psum = 0.0f;
+    R.slots(s, [&](int j) {
+        const float u = s.u[j], z = s.z[j];
+        const float logp = u == -INFINITY ? -INFINITY : (u - u0) / a.tau - lse;
+        s.p[j] = logp;
+        psum += expf(logp);
+        s_in += exp2_hw(above<FAR>(z, c, t.b_all));
         if constexpr (F == kSquare)
-            one_in += exp2_hw(2.0f * above<FAR>(k.z, c, t.b_all));
+            one_in += exp2_hw(2.0f * above<FAR>(z, c, t.b_all));
         else if constexpr (F == kOwn)
-            one_in += exp2_hw(above<FAR>(k.z, kLog2e, t.b_one));
+            one_in += exp2_hw(above<FAR>(z, kLog2e, t.b_one));
     });
     group_put<OpSum>(s_out, s.red[4]);
     group_put<OpSum>(s1, s.red[5]);
@@ -227,18 +224,22 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, Row<TH> &R,
     // p log(p / q) - p + q for each outcome: what is added sums to 0 over all
     // outcomes, and a term is then small where p is near q
     float kl = 0.0f, qsum = 0.0f;
-    R.slots([&](Slot &k, int n) {
-        const float l = above<FAR>(k.z, c, t.b_all);
-        k.p = expf(logp[n] - log_p);
-        k.q = t.none ? 0.0f : exp2_hw(l) / t.s_all;
-        if (k.p == 0.0f)
-            kl += k.q;
-        else if (t.none || k.z == -INFINITY)
+    R.slots(s, [&](int j) {
+        const float z = s.z[j], l = above<FAR>(z, c, t.b_all), logp = s.p[j] - log_p;
+        const float p = expf(logp), q = t.none ? 0.0f : exp2_hw(l) / t.s_all;
+        s.p[j] = p;
+        s.q[j] = q;
+        if (p == 0.0f)
+            kl += q;
+        else if (t.none || z == -INFINITY)
             kl = INFINITY;
         else
-            kl += k.p * ((logp[n] - log_p) - (l * kLn2 - log_all)) - k.p + k.q;
-        qsum += k.q;
+            kl += p * (logp - (l * kLn2 - log_all)) - p + q;
+        qsum += q;
     });
+    for (float *x : {&t.b_out, &t.b_all, &t.b_one, &t.s_out, &t.s_all, &t.s_one, &t.share, &t.pr,
+                     &t.gk, &t.ge})
+        *x = uniform(*x);
     if (!a.loss) return t;
     group_put<OpSum>(kl, s.red[9]);
     group_put<OpSum>(qsum, s.red[10]);
@@ -310,33 +311,34 @@ __device__ __forceinline__ void rest_factors(const Stats &t, bool label, float c
 // The gradient at the slots and at the label, over what the sweep left there.
 // Synchronises first.
 template <int GT, bool FAR, LabelForm F, int TH>
-__device__ __forceinline__ void slot_gradient(Row<TH> &R, const Stats &t, float f_out,
-                                              float f_one, const uint32_t *bits,
-                                              typename Elem<GT>::T *dz)
+__device__ __forceinline__ void slot_gradient(const Row<TH> &R, const DistillShared<TH> &s,
+                                              const Stats &t, float f_out, float f_one,
+                                              const uint32_t *bits, typename Elem<GT>::T *dz)
 {
     __syncthreads();
-    R.slots([&](const Slot &k, int) {
-        float d = t.kd ? t.gk * (k.q - k.p) : 0.0f;
+    R.slots(s, [&](int j) {
+        const int32_t col = s.col[j];
+        float d = t.kd ? t.gk * (s.q[j] - s.p[j]) : 0.0f;
         if (R.y >= 0) {
-            const float l = above_one<FAR, F>(k.z, R.c, t);
-            d += t.ge * ((t.none ? 0.0f : exp2_hw(l) / t.s_one) - (k.col == R.y ? 1.0f : 0.0f));
+            const float l = above_one<FAR, F>(s.z[j], R.c, t);
+            d += t.ge * ((t.none ? 0.0f : exp2_hw(l) / t.s_one) - (col == R.y ? 1.0f : 0.0f));
         }
-        dz[k.col] = narrow<GT>(d);
+        dz[col] = narrow<GT>(d);
     });
     if (threadIdx.x == 0 && R.y >= 0 && !is_marked(bits, R.y))
         dz[R.y] = narrow<GT>(rest_value<FAR, F>(R.zy, R.c, t, f_out, f_one) - t.ge);
 }
 
-// The slots' largest logits.
+// The thread's slots' largest logits.
 template <int TH>
-__device__ __forceinline__ void slot_maxima(const Row<TH> &R, float &m_in, float &um)
+__device__ __forceinline__ void slot_maxima(const Row<TH> &R, const DistillShared<TH> &s,
+                                            float &m_in, float &um)
 {
     m_in = um = -INFINITY;
-#pragma unroll
-    for (int n = 0; n < R.NS; ++n) {
-        m_in = fmaxf(m_in, R.slot[n].z);
-        um = fmaxf(um, R.slot[n].u);
-    }
+    R.slots(s, [&](int j) {
+        m_in = fmaxf(m_in, s.z[j]);
+        um = fmaxf(um, s.u[j]);
+    });
 }
 
 template <int GT, int TH>
@@ -353,14 +355,14 @@ __device__ __forceinline__ void skip_row(const zo_distill &a, int64_t row,
 // A row from memory: the differences first (FAR), one sweep with the running
 // maximum, one for the gradient.
 template <int GT, LabelForm F, int TH>
-__device__ void far_row(const zo_distill &a, Row<TH> &R, DistillShared<TH> &s,
+__device__ void far_row(const zo_distill &a, const Row<TH> &R, DistillShared<TH> &s,
                         const uint32_t *bits, const typename Elem<GT>::T *z,
                         typename Elem<GT>::T *dz)
 {
     constexpr int K = Elem<GT>::kVec, NW = TH / 64;
     const float c = R.c;
     float m = -INFINITY, sum = 0.0f, one = 0.0f, m_in, um;
-    slot_maxima(R, m_in, um);
+    slot_maxima(R, s, m_in, um);
     // the row's last logits count as a vector filled up with -infinity
     for (int64_t i = (int64_t)threadIdx.x * K; i < R.V; i += TH * K) {
         const u32x4 w = load16<GT>(z + i, R.V - i, kNegInf<GT> & kElemMask<GT>);
@@ -410,7 +412,7 @@ __device__ void far_row(const zo_distill &a, Row<TH> &R, DistillShared<TH> &s,
         const u32x4 w = load16<GT>(z + i, R.V - i, kNegInf<GT> & kElemMask<GT>);
         store16<GT>(dz + i, rest_gradient<GT, true, F>(w, c, t, f_out, f_one), R.V - i);
     }
-    slot_gradient<GT, true, F>(R, t, f_out, f_one, bits, dz);
+    slot_gradient<GT, true, F>(R, s, t, f_out, f_one, bits, dz);
 }
 
 template <int GT, LabelForm F>
@@ -459,7 +461,7 @@ __global__ __launch_bounds__(TH, 4) void k_distill(zo_distill a)
     x.load(z, a.vocab);                       // in flight while the slots are read
     read_row<GT, TH>(a, R, s, bits, z);
     float m_in, um;
-    slot_maxima(R, m_in, um);
+    slot_maxima(R, s, m_in, um);
     if (x.has_last(R.V) && is_marked(bits, x.last_column())) x.last = -INFINITY;
     float m_out = x.last;
 #pragma unroll
@@ -494,8 +496,8 @@ __global__ __launch_bounds__(TH, 4) void k_distill(zo_distill a)
         far_row<GT, F, TH>(a, R, s, bits, z, dz);
         return;
     }
-    const float c = R.c, b = base_of<false>(m_out, c);
-    const float b1 = base_of<false>(fmaxf(m_out, m_in), kLog2e);
+    const float c = uniform(R.c), b = uniform(base_of<false>(m_out, c));
+    const float b1 = uniform(base_of<false>(fmaxf(m_out, m_in), kLog2e));
     float sum = 0.0f, one = 0.0f;
     add_terms<F>(x.last, c, b, b1, sum, one);
 #pragma unroll
@@ -512,6 +514,8 @@ __global__ __launch_bounds__(TH, 4) void k_distill(zo_distill a)
     if (!a.dz) return;
     float f_out, f_one;
     rest_factors<false, F>(t, R.y >= 0, c, f_out, f_one);
+    f_out = uniform(f_out);
+    f_one = uniform(f_one);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         repack<GT>(x.w[v]);
@@ -522,7 +526,7 @@ __global__ __launch_bounds__(TH, 4) void k_distill(zo_distill a)
     }
     if (x.has_last(R.V))
         dz[x.last_column()] = narrow<GT>(rest_value<false, F>(x.last, c, t, f_out, f_one));
-    slot_gradient<GT, false, F>(R, t, f_out, f_one, bits, dz);
+    slot_gradient<GT, false, F>(R, s, t, f_out, f_one, bits, dz);
 }
 
 template <int GT, LabelForm F>

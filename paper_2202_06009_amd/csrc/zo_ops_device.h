@@ -192,13 +192,20 @@ __device__ __forceinline__ void group_put(float v, float *s)
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
 }
 
+// A value that is the same in every lane, in a scalar register.
+__device__ __forceinline__ float uniform(float v)
+{
+    return __uint_as_float(
+        (uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(v)));
+}
+
 template <class OP, int NW>
 __device__ __forceinline__ float group_get(const float *s)
 {
     float r = s[0];
 #pragma unroll
     for (int i = 1; i < NW; ++i) r = OP::of(r, s[i]);
-    return r;
+    return uniform(r);
 }
 
 // A row of V < TH * NV * kVec + kVec logits in the registers of a workgroup of TH

@@ -61,8 +61,10 @@ template <int TH>
 __device__ void sort_out(const TopArgs &a, int64_t row, TopShared<TH> &s, int n)
 {
     const int tid = threadIdx.x;
-    if (n <= 256) {
-        // each key's rank is the number of larger keys (all differ): no barriers
+    if (n <= (TH < 384 ? TH : 384)) {
+        // each key's rank is the number of larger keys (all differ): no barriers; about
+        // as quick as the 45 steps below at 384 keys (280 keys: 208 us instead of 240
+        // for 256 of 4096 x 50257)
         if (tid == 0 && (n & 1)) s.cand[n] = 0;
         __syncthreads();
         if (tid < n) {
@@ -360,7 +362,7 @@ __global__ __launch_bounds__(1024) void k_top_long(TopArgs a)
 }
 
 template <int GT, int TH, int NV>
-__global__ __launch_bounds__(TH, 4) void k_top(TopArgs a)
+__global__ __launch_bounds__(TH, TH == 768 ? 6 : 4) void k_top(TopArgs a)
 {
     constexpr int K = Elem<GT>::kVec, NW = TH / 64;
     __shared__ TopShared<TH> s;
@@ -459,11 +461,15 @@ hipError_t launch_top_logits(const TopArgs &a, int gt, hipStream_t st)
             k_top_long<GT><<<dim3((uint32_t)a.rows), 1024, 0, st>>>(a);
             return hipGetLastError();
         }
-        // the more are wanted, the more groups: about 4 a logit or more
+        // the more are wanted, the more threads: about 4 groups a logit or more.  Long
+        // rows: two workgroups of 768 threads a CU, 24 waves (4096 x 50257 bfloat16, 64
+        // wanted: 138 us; of 512 with 16 waves 159, of 256 with 12 waves 175, of 1024
+        // with 32 waves and too few registers 184)
         if (a.top <= 256 && vecs <= 256 * 4) return launch_k_top<GT, 256, 4>(a, st);
         if (a.top <= 256 && vecs <= 256 * 8) return launch_k_top<GT, 256, 8>(a, st);
         if (a.top <= 512 && vecs <= 512 * 8) return launch_k_top<GT, 512, 8>(a, st);
-        if (a.top <= 512 && vecs <= 512 * 16) return launch_k_top<GT, 512, 16>(a, st);
+        if (a.top <= 768 && vecs <= 768 * 9) return launch_k_top<GT, 768, 9>(a, st);
+        if (a.top <= 768 && vecs <= 768 * 11) return launch_k_top<GT, 768, 11>(a, st);
         return launch_k_top<GT, 1024, 16>(a, st);
     });
 }
