@@ -100,9 +100,6 @@ int zo_mx4_linear(const void *x, int32_t dtype, int64_t ldx, const zo_mx4 *w,
                   const zo_mx4 *xq, void *out, int32_t out_dtype, int64_t ldo,
                   hipStream_t stream);
 
-/* Workspace of zo_top_logits in bytes (may be 0), or a negative status. */
-int64_t zo_top_logits_ws(int64_t rows, int64_t vocab, int32_t top);
-
 /*
  * zo_top_logits -- of every row of z [rows, vocab], its `top` largest logits
  * in descending order, the columns they stand in, and the row's log-sum-exp:
@@ -112,12 +109,10 @@ int64_t zo_top_logits_ws(int64_t rows, int64_t vocab, int32_t top);
  * orders above +infinity.  A row of only -infinity has lse = -infinity, one
  * with a NaN has lse = NaN.  top in [1, min(vocab, 1024)], vocab < 2^31,
  * tau > 0 and finite.
- *   ws       device, 16-byte aligned, ws_bytes >= zo_top_logits_ws(rows,
- *            vocab, top); may be NULL when that is 0.
  */
 int zo_top_logits(const void *z, int32_t dtype, int64_t rows, int64_t vocab, int64_t ld,
                   int32_t top, float tau, float *values, int32_t *columns, float *lse,
-                  void *ws, int64_t ws_bytes, hipStream_t stream);
+                  hipStream_t stream);
 
 /*
  * Arguments of zo_distill_loss (host struct, read during the call).
@@ -134,8 +129,6 @@ int zo_top_logits(const void *z, int32_t dtype, int64_t rows, int64_t vocab, int
  *   loss         NULL, or float [rows].
  *   dz           NULL, or [rows, vocab] of z's type, row stride lddz; may be z
  *                itself (with lddz = ldz).
- *   ws           device, 16-byte aligned, ws_bytes >= zo_distill_ws(rows,
- *                vocab); may be NULL when that is 0.
  * top in [1, 1024], vocab in [1, 2^18].
  */
 typedef struct zo_distill {
@@ -152,12 +145,7 @@ typedef struct zo_distill {
     float *loss;
     void *dz;
     int64_t lddz;
-    void *ws;
-    int64_t ws_bytes;
 } zo_distill;
-
-/* Workspace of zo_distill_loss in bytes (may be 0), or a negative status. */
-int64_t zo_distill_ws(int64_t rows, int64_t vocab);
 
 /*
  * zo_distill_loss -- per row, with q = softmax(z / tau), S the columns of the

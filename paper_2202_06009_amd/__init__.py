@@ -32,8 +32,8 @@ EXPORTS = (
     "zo_diag_server_pattern",
     "zo_config_check", "zo_plan_num_chunks", "zo_plan_chunks",
     "zo_mx4_code_bytes", "zo_mx4_scale_bytes", "zo_mx4_quantize", "zo_mx4_dequantize",
-    "zo_mx4_product", "zo_mx4_linear", "zo_top_logits_ws", "zo_top_logits", "zo_distill_ws",
-    "zo_distill_loss", "zo_ops_last_hip_error",
+    "zo_mx4_product", "zo_mx4_linear", "zo_top_logits", "zo_distill_loss",
+    "zo_ops_last_hip_error",
 )
 
 
@@ -73,8 +73,7 @@ class _Distill(ctypes.Structure):
                 ("teacher_lse", ctypes.c_void_p), ("labels", ctypes.c_void_p),
                 ("row_weight", ctypes.c_void_p), ("tau", ctypes.c_float),
                 ("kd_weight", ctypes.c_float), ("ce_weight", ctypes.c_float),
-                ("loss", ctypes.c_void_p), ("dz", ctypes.c_void_p), ("lddz", ctypes.c_int64),
-                ("ws", ctypes.c_void_p), ("ws_bytes", ctypes.c_int64)]
+                ("loss", ctypes.c_void_p), ("dz", ctypes.c_void_p), ("lddz", ctypes.c_int64)]
 
 
 _lib = None
@@ -129,9 +128,7 @@ def lib():
             "zo_mx4_dequantize": ([vp, vp, i32, i64, vp], ci),
             "zo_mx4_product": ([vp, vp, vp, i32, i64, vp], ci),
             "zo_mx4_linear": ([vp, i32, i64, vp, vp, vp, i32, i64, vp], ci),
-            "zo_top_logits_ws": ([i64, i64, i32], i64),
-            "zo_top_logits": ([vp, i32, i64, i64, i64, i32, f32, vp, vp, vp, vp, i64, vp], ci),
-            "zo_distill_ws": ([i64, i64], i64),
+            "zo_top_logits": ([vp, i32, i64, i64, i64, i32, f32, vp, vp, vp, vp], ci),
             "zo_distill_loss": ([ctypes.POINTER(_Distill), vp], ci),
             "zo_ops_last_hip_error": ([], ctypes.c_char_p),
         }
@@ -511,6 +508,6 @@ class ZoAdam:
         return c.value
 
 
-from .operators import (Mx4, zo_distill_loss, zo_distill_ws, zo_mx4_code_bytes,  # noqa: E402
-                        zo_mx4_dequantize, zo_mx4_linear, zo_mx4_product, zo_mx4_quantize,
-                        zo_mx4_scale_bytes, zo_top_logits, zo_top_logits_ws)
+from .operators import (Mx4, zo_distill_loss, zo_mx4_code_bytes, zo_mx4_dequantize,  # noqa: E402
+                        zo_mx4_linear, zo_mx4_product, zo_mx4_quantize, zo_mx4_scale_bytes,
+                        zo_top_logits)

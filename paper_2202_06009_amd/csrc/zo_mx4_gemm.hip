@@ -77,16 +77,21 @@ __device__ __forceinline__ void store_pair(typename Elem<GT>::T *row, int64_t n,
 // of which has an L2 of its own: an XCD gets a contiguous run of tiles, walked
 // down kBand rows of tiles at a time, so that its workgroups share operands.
 constexpr uint32_t kXcds = 8, kBand = 8;
+constexpr int64_t kCus = 256;
 
 struct TileIndex {
     uint32_t m, n;
 };
 
-__device__ __forceinline__ TileIndex tile_index(uint32_t wg, uint32_t m_tiles, uint32_t n_tiles)
+// Workgroup wg of `total` in an XCD's run.
+__device__ __forceinline__ uint32_t run_index(uint32_t wg, uint32_t total)
 {
-    const uint32_t total = m_tiles * n_tiles;
     const uint32_t each = total / kXcds, more = total % kXcds, x = wg % kXcds;
-    const uint32_t id = x * each + min(x, more) + wg / kXcds;
+    return x * each + min(x, more) + wg / kXcds;
+}
+
+__device__ __forceinline__ TileIndex tile_index(uint32_t id, uint32_t m_tiles, uint32_t n_tiles)
+{
     const uint32_t band = id / (kBand * n_tiles), in = id % (kBand * n_tiles);
     const uint32_t height = min(kBand, m_tiles - band * kBand);
     return {band * kBand + in % height, in / height};
@@ -119,23 +124,20 @@ __device__ __forceinline__ const uint8_t *scales_at(const Mx4View &x, int64_t gr
 // to the buffer after that, and loads into their registers are issued: two steps
 // of loads are in flight, about what the memory's latency takes.
 // ODD: an odd number of steps (the register sets go round by twos).
+//
+// The outputs begin at row tile m_tile and column tile n_tile (of 16).
 template <int GT, int MT, int NT, int WN, bool ODD>
-__global__ __launch_bounds__(128 * WN, 2) void k_mx4_product(
-    Mx4View a, Mx4View b, typename Elem<GT>::T *__restrict__ out, int64_t ld, uint32_t m_tiles,
-    uint32_t n_tiles)
+__device__ __forceinline__ void product_tile(const Mx4View &a, const Mx4View &b,
+                                             typename Elem<GT>::T *__restrict__ out, int64_t ld,
+                                             int64_t m_tile, int64_t n_tile, u32x4 *lds)
 {
-    static_assert(MT / 2 <= NT, "a row tile's fragment is read per column tile");
     static_assert(MT % 4 == 0 && NT % 4 == 0, "whole groups of 64 rows per wave");
     constexpr int CHUNKS = 2 * MT + WN * NT, WAVES = 2 * WN;     // 1 KiB tiles of a step
     constexpr int MINE = CHUNKS / WAVES;
     constexpr int MS = MT / 4, NS = NT / 4, HALF = MT / 2;
-    extern __shared__ u32x4 lds[];                               // [3][CHUNKS][64]
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
-    const TileIndex tile = tile_index(blockIdx.x, m_tiles, n_tiles);
-    const int64_t m_tile = (int64_t)tile.m * 2 * MT;             // in tiles of 16
-    const int64_t n_tile = (int64_t)tile.n * WN * NT;
     const int steps = (int)a.kt;
 
     // this wave's share of the loads: chunk c < 2 MT is of a, the others of b
@@ -256,6 +258,45 @@ __global__ __launch_bounds__(128 * WN, 2) void k_mx4_product(
     }
 }
 
+// One tile a workgroup.
+template <int GT, int MT, int NT, int WN, bool ODD>
+__global__ __launch_bounds__(128 * WN, 2) void k_mx4_product(
+    Mx4View a, Mx4View b, typename Elem<GT>::T *__restrict__ out, int64_t ld, uint32_t m_tiles,
+    uint32_t n_tiles)
+{
+    extern __shared__ u32x4 lds[];                               // [3][CHUNKS][64]
+    const TileIndex tile = tile_index(run_index(blockIdx.x, m_tiles * n_tiles), m_tiles, n_tiles);
+    product_tile<GT, MT, NT, WN, ODD>(a, b, out, ld, (int64_t)tile.m * 2 * MT,
+                                      (int64_t)tile.n * WN * NT, lds);
+}
+
+// Tiles of 256 x 256, of which the first `whole` take one workgroup each and the
+// others, too few for a round of the GPU, two of 128 rows each.
+template <int GT, bool ODD>
+__global__ __launch_bounds__(512, 2) void k_mx4_product_large(
+    Mx4View a, Mx4View b, typename Elem<GT>::T *__restrict__ out, int64_t ld, uint32_t m_tiles,
+    uint32_t n_tiles, uint32_t whole)
+{
+    extern __shared__ u32x4 lds[];
+    if (blockIdx.x < whole) {
+        const TileIndex tile = tile_index(run_index(blockIdx.x, whole), m_tiles, n_tiles);
+        product_tile<GT, 8, 4, 4, ODD>(a, b, out, ld, (int64_t)tile.m * 16, (int64_t)tile.n * 16,
+                                       lds);
+    } else {
+        const uint32_t half = blockIdx.x - whole;
+        const TileIndex tile = tile_index(whole + half / 2, m_tiles, n_tiles);
+        product_tile<GT, 4, 4, 4, ODD>(a, b, out, ld, (int64_t)tile.m * 16 + half % 2 * 8,
+                                       (int64_t)tile.n * 16, lds);
+    }
+}
+
+// Shared memory beyond 64 KiB has to be asked for.
+static hipError_t allow_lds(const void *kernel, uint32_t lds)
+{
+    if (lds <= 65536) return hipSuccess;
+    return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+}
+
 template <int GT, int MT, int NT, int WN>
 static hipError_t launch_tiles(const Mx4View &a, const Mx4View &b, void *out, int64_t ld,
                                hipStream_t st)
@@ -266,14 +307,28 @@ static hipError_t launch_tiles(const Mx4View &a, const Mx4View &b, void *out, in
     if (tiles > INT32_MAX || a.kt > INT32_MAX) return hipErrorInvalidValue;
     const auto kernel =
         a.kt % 2 ? k_mx4_product<GT, MT, NT, WN, true> : k_mx4_product<GT, MT, NT, WN, false>;
-    if (lds > 65536) {
-        const hipError_t e = hipFuncSetAttribute(
-            reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-            (int)lds);
-        if (e != hipSuccess) return e;
-    }
+    const hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), lds);
+    if (e != hipSuccess) return e;
     kernel<<<dim3((uint32_t)tiles), 128 * WN, lds, st>>>(
         a, b, static_cast<typename Elem<GT>::T *>(out), ld, (uint32_t)mt, (uint32_t)nt);
+    return hipGetLastError();
+}
+
+template <int GT>
+static hipError_t launch_large(const Mx4View &a, const Mx4View &b, void *out, int64_t ld,
+                               hipStream_t st)
+{
+    constexpr uint32_t lds = 3 * 32 * 1024;
+    const int64_t mt = (a.rows + 255) / 256, nt = (b.rows + 255) / 256, tiles = mt * nt;
+    if (tiles > INT32_MAX || a.kt > INT32_MAX) return hipErrorInvalidValue;
+    const int64_t rest = tiles % kCus;
+    const int64_t whole = rest <= kCus / 2 && tiles > kCus ? tiles - rest : tiles;
+    const auto kernel = a.kt % 2 ? k_mx4_product_large<GT, true> : k_mx4_product_large<GT, false>;
+    const hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), lds);
+    if (e != hipSuccess) return e;
+    kernel<<<dim3((uint32_t)(whole + 2 * (tiles - whole))), 512, lds, st>>>(
+        a, b, static_cast<typename Elem<GT>::T *>(out), ld, (uint32_t)mt, (uint32_t)nt,
+        (uint32_t)whole);
     return hipGetLastError();
 }
 
@@ -287,7 +342,7 @@ hipError_t launch_mx4_product(const Mx4View &a, const Mx4View &b, void *out, int
     };
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
-        if (count(256, 256) >= 224) return launch_tiles<GT, 8, 4, 4>(a, b, out, ld, st);
+        if (count(256, 256) >= 224) return launch_large<GT>(a, b, out, ld, st);
         if (count(128, 128) >= 144) return launch_tiles<GT, 4, 4, 2>(a, b, out, ld, st);
         return launch_tiles<GT, 4, 4, 1>(a, b, out, ld, st);
     });

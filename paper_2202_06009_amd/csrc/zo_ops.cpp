@@ -146,36 +146,21 @@ int zo_mx4_linear(const void *x, int32_t dtype, int64_t ldx, const zo_mx4 *w, co
     return from_hip(zo::launch_mx4_product(v, view(w), out, go, ldo, stream));
 }
 
-int64_t zo_top_logits_ws(int64_t rows, int64_t vocab, int32_t top)
-{
-    if (rows < 0 || rows > INT32_MAX || vocab < 1 || vocab > INT32_MAX || top < 1 ||
-        top > 1024 || top > vocab)
-        return ZO_EINVAL;
-    return 0;
-}
-
 int zo_top_logits(const void *z, int32_t dtype, int64_t rows, int64_t vocab, int64_t ld,
-                  int32_t top, float tau, float *values, int32_t *columns, float *lse, void *ws,
-                  int64_t ws_bytes, hipStream_t stream)
+                  int32_t top, float tau, float *values, int32_t *columns, float *lse,
+                  hipStream_t stream)
 {
     const int gt = elem(dtype);
-    const int64_t need = zo_top_logits_ws(rows, vocab, top);
-    if (need < 0) return (int)need;
+    if (rows < 0 || rows > INT32_MAX || vocab < 1 || vocab > INT32_MAX) return ZO_EINVAL;
+    if (top < 1 || top > 1024 || top > vocab) return ZO_EINVAL;
     if (gt < 0 || !(tau > 0.0f) || !std::isfinite(tau)) return ZO_EINVAL;
     if (rows == 0) return ZO_OK;
     if (!z || ld < vocab || ld > kMaxLd || !values || !columns) return ZO_EINVAL;
-    if (need && (!ws || ws_bytes < need)) return ZO_EINVAL;
     if (!aligned(z, gt == zo::GT_F32 ? 4 : 2) || !aligned(values, 4) || !aligned(columns, 4) ||
-        !aligned(lse, 4) || !aligned(ws, 16))
+        !aligned(lse, 4))
         return ZO_EALIGN;
-    const zo::TopArgs a = {z, rows, vocab, ld, top, tau, values, columns, lse, ws};
+    const zo::TopArgs a = {z, rows, vocab, ld, top, tau, values, columns, lse};
     return from_hip(zo::launch_top_logits(a, gt, stream));
-}
-
-int64_t zo_distill_ws(int64_t rows, int64_t vocab)
-{
-    if (rows < 0 || rows > INT32_MAX || vocab < 1 || vocab > (1 << 18)) return ZO_EINVAL;
-    return 0;
 }
 
 int zo_distill_loss(const zo_distill *args, hipStream_t stream)
@@ -183,8 +168,7 @@ int zo_distill_loss(const zo_distill *args, hipStream_t stream)
     if (!args) return ZO_EINVAL;
     const zo_distill &a = *args;
     const int gt = elem(a.dtype);
-    const int64_t need = zo_distill_ws(a.rows, a.vocab);
-    if (need < 0) return (int)need;
+    if (a.rows < 0 || a.rows > INT32_MAX || a.vocab < 1 || a.vocab > (1 << 18)) return ZO_EINVAL;
     if (gt < 0 || a.top < 1 || a.top > 1024) return ZO_EINVAL;
     if (!(a.tau > 0.0f) || !std::isfinite(a.tau) || !std::isfinite(a.kd_weight) ||
         !std::isfinite(a.ce_weight))
@@ -194,11 +178,10 @@ int zo_distill_loss(const zo_distill *args, hipStream_t stream)
     if (!a.loss && !a.dz) return ZO_EINVAL;
     if (a.dz && (a.lddz < a.vocab || a.lddz > kMaxLd || (a.dz == a.z && a.lddz != a.ldz)))
         return ZO_EINVAL;
-    if (need && (!a.ws || a.ws_bytes < need)) return ZO_EINVAL;
     const uintptr_t ea = gt == zo::GT_F32 ? 4 : 2;
     if (!aligned(a.z, ea) || !aligned(a.dz, ea) || !aligned(a.values, 4) ||
         !aligned(a.columns, 4) || !aligned(a.teacher_lse, 4) || !aligned(a.labels, 4) ||
-        !aligned(a.row_weight, 4) || !aligned(a.loss, 4) || !aligned(a.ws, 16))
+        !aligned(a.row_weight, 4) || !aligned(a.loss, 4))
         return ZO_EALIGN;
     return from_hip(zo::launch_distill(a, stream));
 }

@@ -39,7 +39,6 @@ struct TopArgs {
     float *values;
     int32_t *columns;
     float *lse;
-    void *ws;
 };
 hipError_t launch_top_logits(const TopArgs &a, int gt, hipStream_t st);
 hipError_t launch_distill(const zo_distill &a, hipStream_t st);

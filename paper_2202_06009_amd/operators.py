@@ -36,16 +36,6 @@ def zo_mx4_scale_bytes(rows, cols):
     return _size(lib().zo_mx4_scale_bytes(int(rows), int(cols)), "zo_mx4_scale_bytes")
 
 
-def zo_top_logits_ws(rows, vocab, top):
-    """Bytes of workspace of zo_top_logits."""
-    return _size(lib().zo_top_logits_ws(int(rows), int(vocab), int(top)), "zo_top_logits_ws")
-
-
-def zo_distill_ws(rows, vocab):
-    """Bytes of workspace of zo_distill_loss."""
-    return _size(lib().zo_distill_ws(int(rows), int(vocab)), "zo_distill_ws")
-
-
 class Mx4:
     """A rows x cols matrix in microscaled 4-bit floating point: ``codes`` and
     ``scales``, uint8 device tensors in the layout of ``zo_mx4`` (allocated when
@@ -132,19 +122,6 @@ def _mx4(q, what, dev):
     return q._at
 
 
-def _workspace(ws, nbytes, dev, stream):
-    """The caller's workspace, or one from torch's allocator on the call's stream."""
-    if nbytes == 0:
-        return None
-    if ws is None:
-        with torch.cuda.stream(stream):
-            return torch.empty(nbytes, dtype=torch.uint8, device=dev)
-    if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.numel() < nbytes:
-        raise ValueError(f"ws: needs {nbytes} contiguous uint8 elements")
-    _at(ws, "ws", dev)
-    return ws
-
-
 _functions = {}
 
 
@@ -208,7 +185,7 @@ def zo_mx4_linear(x, w, out, xq, stream=None):
     _run("zo_mx4_linear", dev, stream, (px, dx, ldx, pw, pq, po, do, ldo), (x, w, out, xq))
 
 
-def zo_top_logits(z, values, columns, lse=None, *, tau=1.0, ws=None, stream=None):
+def zo_top_logits(z, values, columns, lse=None, *, tau=1.0, stream=None):
     """The values.shape[1] largest logits of every row of z [rows, vocab] in
     descending order (ties: lowest column first) into values (float32), their
     columns into columns (int32), and log sum exp(z / tau) into lse [rows]."""
@@ -221,16 +198,12 @@ def zo_top_logits(z, values, columns, lse=None, *, tau=1.0, ws=None, stream=None
     pv = _vector(values, "values", dev, torch.float32, (rows, top))
     pc = _vector(columns, "columns", dev, torch.int32, (rows, top))
     pl = _vector(lse, "lse", dev, torch.float32, (rows,))
-    ws = _workspace(ws, zo_top_logits_ws(rows, vocab, top), dev, stream)
-    pw, nw = (None, 0) if ws is None else (ws.data_ptr(), ws.numel())
-    _run("zo_top_logits", dev, stream,
-         (p, dt, rows, vocab, ld, top, float(tau), pv, pc, pl, pw, nw),
-         (z, values, columns, lse, ws))
+    _run("zo_top_logits", dev, stream, (p, dt, rows, vocab, ld, top, float(tau), pv, pc, pl),
+         (z, values, columns, lse))
 
 
 def zo_distill_loss(z, values, columns, loss=None, dz=None, *, tau=1.0, teacher_lse=None,
-                    labels=None, kd_weight=1.0, ce_weight=0.0, row_weight=None, ws=None,
-                    stream=None):
+                    labels=None, kd_weight=1.0, ce_weight=0.0, row_weight=None, stream=None):
     """Distillation from a teacher's top logits: the loss of every row of the
     student's logits z [rows, vocab] into loss (float32 [rows]) and / or its
     gradient into dz (z's type and shape; may be z itself).
@@ -251,8 +224,6 @@ def zo_distill_loss(z, values, columns, loss=None, dz=None, *, tau=1.0, teacher_
         if dz.dtype != z.dtype:
             raise ValueError(f"dz: expected {z.dtype}, got {dz.dtype}")
         pdz, _, lddz = _matrix(dz, "dz", dev, rows, vocab)
-    ws = _workspace(ws, zo_distill_ws(rows, vocab), dev, stream)
-    pw, nw = (None, 0) if ws is None else (ws.data_ptr(), ws.numel())
     a = _Distill(p, dt, rows, vocab, ldz, top,
                  _vector(values, "values", dev, torch.float32, (rows, top)),
                  _vector(columns, "columns", dev, torch.int32, (rows, top)),
@@ -260,6 +231,6 @@ def zo_distill_loss(z, values, columns, loss=None, dz=None, *, tau=1.0, teacher_
                  _vector(labels, "labels", dev, torch.int32, (rows,)),
                  _vector(row_weight, "row_weight", dev, torch.float32, (rows,)),
                  float(tau), float(kd_weight), float(ce_weight),
-                 _vector(loss, "loss", dev, torch.float32, (rows,)), pdz, lddz, pw, nw)
+                 _vector(loss, "loss", dev, torch.float32, (rows,)), pdz, lddz)
     _run("zo_distill_loss", dev, stream, (ctypes.byref(a),),
-         (z, values, columns, teacher_lse, labels, row_weight, loss, dz, ws))
+         (z, values, columns, teacher_lse, labels, row_weight, loss, dz))

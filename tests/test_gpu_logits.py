@@ -118,11 +118,9 @@ def test_top_without_lse_on_a_stream_and_in_a_graph(torch):
         zo.zo_top_logits(z, values, columns, lse, stream=s)
         torch.cuda.current_stream().wait_stream(s)
         _check_top(torch, z, 9, got=(values, columns, lse))
-        ws = torch.empty(zo.zo_top_logits_ws(rows, 20011, 9) or 1, dtype=torch.uint8,
-                         device="cuda")
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g):
-            zo.zo_top_logits(z, values, columns, lse, ws=ws)
+            zo.zo_top_logits(z, values, columns, lse)
         for i in range(4):
             z.normal_(std=2.0)
             columns.zero_()
@@ -366,10 +364,9 @@ def test_distill_on_a_stream_and_in_a_graph(torch):
         torch.cuda.current_stream().wait_stream(s)
         again, dz2 = _distill(torch, z, vals, cols, lse=lse)
         assert torch.equal(loss, again) and torch.equal(dz, dz2)
-        ws = torch.empty(zo.zo_distill_ws(rows, 9001) or 1, dtype=torch.uint8, device="cuda")
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g):
-            zo.zo_distill_loss(z, v, c, loss, dz, teacher_lse=l, ws=ws)
+            zo.zo_distill_loss(z, v, c, loss, dz, teacher_lse=l)
         for i in range(4):
             z.normal_()
             loss.zero_()

@@ -167,6 +167,27 @@ def test_product_and_linear(torch, mnk):
         assert (lin[:, n:] == 7.0).all()
 
 
+@pytest.mark.parametrize("m,n,k", [(2300, 7300, 200), (4090, 4100, 60), (2050, 8200, 300)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_product_of_many_tiles(torch, m, n, k, dtype):
+    """More tiles than the GPU has CUs, whole rounds of them and a rest; compared on
+    the GPU in 64 bits."""
+    import paper_2202_06009_amd as zo
+    a = torch.randn((m, k), device="cuda")
+    b = torch.randn((n, k), device="cuda")
+    (aq, _), (bq, _) = _quantized(torch, a, cols=False), _quantized(torch, b, cols=False)
+    va, vb = torch.empty_like(a), torch.empty_like(b)
+    zo.zo_mx4_dequantize(aq, va)
+    zo.zo_mx4_dequantize(bq, vb)
+    out = torch.full((m, n), 7.0, dtype=getattr(torch, dtype), device="cuda")
+    zo.zo_mx4_product(aq, bq, out)
+    va, vb = va.double(), vb.double()
+    want = va @ vb.t().contiguous()
+    acc = (k + 8) * 2.0 ** -23 * (va.abs() @ vb.abs().t().contiguous())
+    assert bool(((out.double() - want).abs()
+                 <= acc + HALF_ULP[dtype] * (want.abs() + acc) + 2.0 ** -134).all())
+
+
 @pytest.mark.parametrize("m", [1, 2, 5, 8, 15, 16, 17, 40, 64, 65, 100])
 @pytest.mark.parametrize("xdtype", ["float32", "float16", "bfloat16"])
 def test_linear_few_rows(torch, m, xdtype):

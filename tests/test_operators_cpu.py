@@ -92,31 +92,19 @@ def test_linear_and_dequantize_refusals():
     (dict(tau=float("inf")), zo.ZO_EINVAL), (dict(ld=99), zo.ZO_EINVAL),
     (dict(dtype=5), zo.ZO_EINVAL), (dict(z=None), zo.ZO_EINVAL),
     (dict(values=None), zo.ZO_EINVAL), (dict(columns=None), zo.ZO_EINVAL),
-    (dict(z=P + 2), zo.ZO_EALIGN), (dict(lse=P + 1), zo.ZO_EALIGN), (dict(ws=P + 8), zo.ZO_EALIGN),
+    (dict(z=P + 2), zo.ZO_EALIGN), (dict(lse=P + 1), zo.ZO_EALIGN),
     (dict(rows=0, z=None, values=None), zo.ZO_OK),
 ])
 def test_top_logits_refusals(over, code):
-    a = dict(z=P, dtype=0, rows=3, vocab=100, ld=100, top=7, tau=1.0, values=P, columns=P, lse=P,
-             ws=P, ws_bytes=1 << 40)
+    a = dict(z=P, dtype=0, rows=3, vocab=100, ld=100, top=7, tau=1.0, values=P, columns=P, lse=P)
     a.update(over)
     assert zo.lib().zo_top_logits(*a.values(), None) == code
-
-
-def test_workspaces_too_small_are_refused():
-    need = zo.zo_top_logits_ws(1, 100000, 7)
-    if need:
-        assert zo.lib().zo_top_logits(P, 0, 1, 100000, 100000, 7, 1.0, P, P, P, P, need - 1,
-                                      None) == zo.ZO_EINVAL
-    need = zo.zo_distill_ws(1, 100000)
-    if need:
-        a = _distill(rows=1, vocab=100000, ldz=100000, lddz=100000, ws=P, ws_bytes=need - 1)
-        assert zo.lib().zo_distill_loss(ctypes.byref(a), None) == zo.ZO_EINVAL
 
 
 def _distill(**over):
     a = dict(z=P, dtype=2, rows=3, vocab=100, ldz=100, top=7, values=P, columns=P,
              teacher_lse=None, labels=None, row_weight=None, tau=1.0, kd_weight=1.0,
-             ce_weight=0.0, loss=P, dz=2 * P, lddz=100, ws=P, ws_bytes=1 << 40)
+             ce_weight=0.0, loss=P, dz=2 * P, lddz=100)
     a.update(over)
     return zo._Distill(**a)
 
