@@ -13,16 +13,18 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libzoadam.so")
 CSRC = os.path.join(HERE, "csrc")
+OPS = os.path.join(CSRC, "ops")
 SOURCES = [os.path.join(CSRC, f) for f in ("zo_kernels.hip", "zo_server.hip",
                                            "zo_server_many.hip", "zo_server_ua.hip",
-                                           "zo_kernels_ua.hip", "zo_adam.cpp",
-                                           "zo_mx4_quant.hip", "zo_mx4_gemm.hip",
-                                           "zo_mx4_few.hip",
-                                           "zo_top.hip", "zo_distill.hip", "zo_ops.cpp")]
+                                           "zo_kernels_ua.hip", "zo_adam.cpp")]
+# the operators of zo_ops.h, apart from the optimizer step's kernels
+OPERATORS = [os.path.join(OPS, f) for f in ("zo_mx4_quant.hip", "zo_mx4_gemm.hip",
+                                            "zo_mx4_few.hip", "zo_top.hip", "zo_distill.hip",
+                                            "zo_ops.cpp")]
 HEADERS = [os.path.join(ROOT, "include", "zo_adam.h"), os.path.join(ROOT, "include", "zo_ops.h"),
-           os.path.join(CSRC, "zo_internal.h"), os.path.join(CSRC, "zo_ops_internal.h"),
-           os.path.join(CSRC, "zo_ops_device.h"), os.path.join(CSRC, "zo_mx4_device.h"),
-           os.path.join(CSRC, "zo_device.h"), os.path.join(CSRC, "zo_server.h")]
+           os.path.join(CSRC, "zo_internal.h"), os.path.join(CSRC, "zo_device.h"),
+           os.path.join(CSRC, "zo_server.h"), os.path.join(OPS, "zo_ops_internal.h"),
+           os.path.join(OPS, "zo_ops_device.h"), os.path.join(OPS, "zo_mx4_device.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-ffp-contract=off", "-fno-fast-math",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -36,7 +38,7 @@ def _filter(text):
 def build(verbose: bool = False) -> str:
     with tempfile.TemporaryDirectory(prefix="zoadam_build_") as tmpd:
         objs, procs = [], []
-        for src in SOURCES:
+        for src in SOURCES + OPERATORS:
             obj = os.path.join(tmpd, os.path.basename(src) + ".o")
             cmd = [HIPCC] + FLAGS + ["-c", "-x", "hip", src, "-o", obj]
             if verbose:
