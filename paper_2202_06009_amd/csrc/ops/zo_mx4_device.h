@@ -62,4 +62,19 @@ __device__ __forceinline__ f32x4 mfma(const u32x4 &a, const u32x4 &b, f32x4 acc,
                                                             (int)sb);
 }
 
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// The 32 x 32 x 64 form: lane l holds row l % 32, elements 32 (l / 32) .. + 31; of its
+// sixteen results lane l holds, for b's columns l % 32, a's rows
+// 8 q + 4 (l / 32) + 0..3 at 4 q.
+template <int SA, int SB>
+__device__ __forceinline__ f32x16 mfma32(const u32x4 &a, const u32x4 &b, f32x16 acc, uint32_t sa,
+                                         uint32_t sb)
+{
+    const i32x8 x = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+    const i32x8 y = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc, 4, 4, SA, (int)sa, SB,
+                                                           (int)sb);
+}
+
 }  // namespace zo

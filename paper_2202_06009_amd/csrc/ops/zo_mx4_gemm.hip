@@ -1,15 +1,18 @@
-// zo_mx4_gemm.hip -- products of microscaled 4-bit matrices on the scaled
-// matrix instruction (16 x 16 x 128, E2M1 operands, binary32 accumulators).
+// zo_mx4_gemm.hip -- products of microscaled 4-bit matrices on the scaled matrix
+// instruction (32 x 32 x 64, E2M1 operands, binary32 accumulators).  Of the two forms
+// with 4-bit operands this one gives 8.8 PFLOP/s by itself, the 16 x 16 x 128 one 5.0 to
+// 6.5 (each instruction costs an issue slot more for its scales).
 //
-// Operand layout of the instruction: lane l holds row l % 16, elements
-// 32 (l / 16) .. + 31 of the 128 (16 bytes) and their scale byte, one of the
-// four bytes of a register.  The storage order of an mx4 matrix (zo_ops.h) is
-// that: a tile of 16 rows x 128 columns is the 1 KiB that a wave loads with
-// one 16-byte access per lane, and the scale dword of a lane serves four such
-// tiles, rows 0..63 of a group.
+// Operand layout of the instruction: lane l holds row l % 32, elements
+// 32 (l / 32) .. + 31 of the 64 (16 bytes), and their scale byte, one of the four bytes
+// of a register.  An mx4 matrix (zo_ops.h) keeps these 16 bytes in tiles of 16 rows x
+// 128 columns, block after block of 32 columns: two adjacent tiles hold two fragments
+// of 32 rows x 64 columns, and 16 lanes read 256 contiguous bytes.  A lane's scale
+// dword serves rows r % 16 + 16 {0, 1, 2, 3} of 64: shifted right by 8 in the lanes of
+// the upper 16 rows, its bytes 0 and 2 are those of the two fragments.
 //
-// With b's rows as the first operand, lane l's four results are columns
-// n = 4 (l / 16) .. + 3 of row m = l % 16 of the output.
+// With b's rows as the first operand, a lane's results are runs of four columns of one
+// row of the output.
 #include "zo_mx4_device.h"
 
 namespace zo {
@@ -24,50 +27,50 @@ __device__ __forceinline__ void unroll(F &&f)
     }
 }
 
-// Two adjacent 16 x 16 tiles of results, u of columns n .. n + 15 and v of the next
-// 16: rows of 16 lanes swap halves so that a lane holds 8 consecutive columns (of
-// u in lanes 0..15 and 32..47, of v in the others) and a row of the output gets 64
-// (16-bit) or 128 bytes at once.
+// The 32 columns from n on of a row of results.  16-bit results: the wave's halves
+// swap runs of four, so that a lane holds 8 consecutive columns.
 template <int GT>
-__device__ __forceinline__ void store_pair(typename Elem<GT>::T *row, int64_t n, int64_t cols,
-                                           bool inside, f32x4 u, f32x4 v, int lane)
+__device__ __forceinline__ void store_row(typename Elem<GT>::T *row, int64_t n, int64_t cols,
+                                          bool inside, const f32x16 &v, int half)
 {
-    const int g = lane >> 4;
     if constexpr (GT == GT_F32) {
-        // 16 bytes a lane as they are
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const f32x4 &x = h ? v : u;
-            const int64_t at = n + h * 16 + g * 4, nv = cols - at;
+        for (int q = 0; q < 4; ++q) {
+            const int64_t at = n + q * 8 + half * 4, nv = cols - at;
             if (!inside) continue;
+            const u32x4 w = {__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]),
+                             __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3])};
             if (nv >= 4) {
-                *reinterpret_cast<u32x4_a2 *>(row + at) = __builtin_bit_cast(u32x4, x);
+                *reinterpret_cast<u32x4_a2 *>(row + at) = w;
             } else {
-                for (int q = 0; q < 4; ++q)
-                    if (q < nv) row[at + q] = __float_as_uint(x[q]);
+                for (int e = 0; e < 4; ++e)
+                    if (e < nv) row[at + e] = w[e];
             }
         }
     } else {
-        u32x4 w;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t a = (uint32_t)narrow<GT>(u[2 * h]) |
-                               (uint32_t)narrow<GT>(u[2 * h + 1]) << 16;
-            const uint32_t b = (uint32_t)narrow<GT>(v[2 * h]) |
-                               (uint32_t)narrow<GT>(v[2 * h + 1]) << 16;
-            const auto s = __builtin_amdgcn_permlane16_swap(a, b, false, false);
-            w[h] = s[0];
-            w[2 + h] = s[1];
-        }
-        const int64_t at = n + (g & 1) * 16 + (g >> 1) * 8, nv = cols - at;
-        if (!inside) return;
-        if (nv >= 8) {
-            *reinterpret_cast<u32x4_a2 *>(row + at) = w;
-        } else {
-            for (int q = 0; q < 8; ++q) {
-                if (q >= nv) break;
-                const uint32_t d = q < 2 ? w[0] : q < 4 ? w[1] : q < 6 ? w[2] : w[3];
-                row[at + q] = (uint16_t)(d >> (16 * (q & 1)));
+        for (int q = 0; q < 4; q += 2) {
+            u32x4 w;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t x = (uint32_t)narrow<GT>(v[4 * q + 2 * h]) |
+                                   (uint32_t)narrow<GT>(v[4 * q + 2 * h + 1]) << 16;
+                const uint32_t y = (uint32_t)narrow<GT>(v[4 * q + 4 + 2 * h]) |
+                                   (uint32_t)narrow<GT>(v[4 * q + 5 + 2 * h]) << 16;
+                const auto s = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+                w[h] = s[0];
+                w[2 + h] = s[1];
+            }
+            const int64_t at = n + (q + half) * 8, nv = cols - at;
+            if (!inside) continue;
+            if (nv >= 8) {
+                *reinterpret_cast<u32x4_a2 *>(row + at) = w;
+            } else {
+                for (int e = 0; e < 8; ++e) {
+                    if (e >= nv) break;
+                    const uint32_t d = e < 2 ? w[0] : e < 4 ? w[1] : e < 6 ? w[2] : w[3];
+                    row[at + e] = (uint16_t)(d >> (16 * (e & 1)));
+                }
             }
         }
     }
@@ -125,6 +128,14 @@ __device__ __forceinline__ const uint8_t *scales_at(const Mx4View &x, int64_t gr
 // of loads are in flight, about what the memory's latency takes.
 // ODD: an odd number of steps (the register sets go round by twos).
 //
+// Measured: 16384 x 16384 by 8192 1.13 ms (3.8 PFLOP/s), 8192 x 6400 by 1600 66 us, 8192 x 1600
+// by 6400 53 us.  Bound: copies of the kernel that leave work out (on the 16 x 16 x 128
+// form) took 0.79 ms of 1.12 without any operand traffic, 0.85 without the loads and
+// the writes to shared memory, 1.02 without the reads from it: the loads (32 KiB a
+// step through the L1, about 30 bytes a clock) take the most, the matrix pipe next.
+// Four waves of 128 x 128 read less of shared memory but leave no registers for loads
+// in flight (1.5 ms); workgroups of 128 x 256, two a CU, spill (1.8 ms).
+//
 // The outputs begin at row tile m_tile and column tile n_tile (of 16).
 template <int GT, int MT, int NT, int WN, bool ODD>
 __device__ __forceinline__ void product_tile(const Mx4View &a, const Mx4View &b,
@@ -134,7 +145,8 @@ __device__ __forceinline__ void product_tile(const Mx4View &a, const Mx4View &b,
     static_assert(MT % 4 == 0 && NT % 4 == 0, "whole groups of 64 rows per wave");
     constexpr int CHUNKS = 2 * MT + WN * NT, WAVES = 2 * WN;     // 1 KiB tiles of a step
     constexpr int MINE = CHUNKS / WAVES;
-    constexpr int MS = MT / 4, NS = NT / 4, HALF = MT / 2;
+    constexpr int MS = MT / 4, NS = NT / 4;                      // groups of 64 rows
+    constexpr int MF = MT / 2, NF = NT / 2, HALF = MF / 2;       // fragments of 32 rows
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
@@ -153,9 +165,14 @@ __device__ __forceinline__ void product_tile(const Mx4View &a, const Mx4View &b,
 #pragma unroll
     for (int g = 0; g < NS; ++g) sb[g] = scales_at(b, n_tile / 4 + wn * NS + g);
 
+    // lane's place in a fragment: row half and 32-column block of the 64
+    const int upper = lane >> 4 & 1, block = lane >> 5;
+    const int frag_at = upper * 64 + block * 16 + (lane & 15);
+    const int scale_at = (block * 16 + (lane & 15)) * 4;
+
     // set R holds the tiles and scales of the steps congruent to R modulo 2
     u32x4 stage[2][MINE];
-    uint32_t ea[2][MS], eb[2][NS];
+    uint32_t ea[2][MS][2], eb[2][NS][2];      // the scales of both halves of a column tile
     auto fetch = [&](auto set, int t) {
         constexpr int R = decltype(set)::value;
         const int64_t at = min(t, steps - 1);
@@ -167,11 +184,16 @@ __device__ __forceinline__ void product_tile(const Mx4View &a, const Mx4View &b,
         constexpr int R = decltype(set)::value;
         const int64_t at = min(t, steps - 1);
 #pragma unroll
-        for (int g = 0; g < MS; ++g)
-            ea[R][g] = *reinterpret_cast<const uint32_t *>(sa[g] + at * 256 + lane * 4);
+        for (int p = 0; p < 2; ++p) {
 #pragma unroll
-        for (int g = 0; g < NS; ++g)
-            eb[R][g] = *reinterpret_cast<const uint32_t *>(sb[g] + at * 256 + lane * 4);
+            for (int g = 0; g < MS; ++g)
+                ea[R][g][p] = *reinterpret_cast<const uint32_t *>(sa[g] + at * 256 + p * 128 +
+                                                                  scale_at);
+#pragma unroll
+            for (int g = 0; g < NS; ++g)
+                eb[R][g][p] = *reinterpret_cast<const uint32_t *>(sb[g] + at * 256 + p * 128 +
+                                                                  scale_at);
+        }
     };
     auto put = [&](auto set, int buf) {
         constexpr int R = decltype(set)::value;
@@ -179,23 +201,30 @@ __device__ __forceinline__ void product_tile(const Mx4View &a, const Mx4View &b,
         for (int i = 0; i < MINE; ++i)
             lds[(buf * CHUNKS + i * WAVES + wave) * 64 + lane] = stage[R][i];
     };
-    u32x4 fa[MT], fb[NT];
+    u32x4 fa[MF][2], fb[NF][2];
     auto read_a = [&](int buf, auto i) {
         constexpr int I = decltype(i)::value;
-        fa[I] = lds[(buf * CHUNKS + wm * MT + I) * 64 + lane];
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+            fa[I][p] = lds[(buf * CHUNKS + wm * MT + 2 * I) * 64 + p * 32 + frag_at];
     };
     auto read_b = [&](int buf, auto j) {
         constexpr int J = decltype(j)::value;
-        fb[J] = lds[(buf * CHUNKS + 2 * MT + wn * NT + J) * 64 + lane];
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+            fb[J][p] = lds[(buf * CHUNKS + 2 * MT + wn * NT + 2 * J) * 64 + p * 32 + frag_at];
     };
-    f32x4 acc[MT][NT] = {};
-    // the products of half the row tiles with column tile j
+    f32x16 acc[MF][NF] = {};
+    // the products of half the row fragments with column fragment j
     auto multiply = [&](auto set, auto from, auto j) {
-        unroll<HALF>([&](auto i) {
-            constexpr int R = decltype(set)::value;
-            constexpr int I = decltype(from)::value + decltype(i)::value;
-            constexpr int J = decltype(j)::value;
-            acc[I][J] = mfma<J % 4, I % 4>(fb[J], fa[I], acc[I][J], eb[R][J / 4], ea[R][I / 4]);
+        unroll<2>([&](auto p) {
+            unroll<HALF>([&](auto i) {
+                constexpr int R = decltype(set)::value, P = decltype(p)::value;
+                constexpr int I = decltype(from)::value + decltype(i)::value;
+                constexpr int J = decltype(j)::value;
+                acc[I][J] = mfma32<J % 2 * 2, I % 2 * 2>(fb[J][P], fa[I][P], acc[I][J],
+                                                         eb[R][J / 2][P], ea[R][I / 2][P]);
+            });
         });
     };
     using Zero = std::integral_constant<int, 0>;
@@ -204,19 +233,27 @@ __device__ __forceinline__ void product_tile(const Mx4View &a, const Mx4View &b,
     // step t, t congruent to `now` modulo 2, in buffer t modulo 3
     int buf = 0;
     auto step = [&](auto now, int t) {
+        constexpr int R = decltype(now)::value;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+#pragma unroll
+            for (int g = 0; g < MS; ++g) ea[R][g][p] >>= upper * 8;
+#pragma unroll
+            for (int g = 0; g < NS; ++g) eb[R][g][p] >>= upper * 8;
+        }
         const int next = buf == 2 ? 0 : buf + 1, after = next == 2 ? 0 : next + 1;
-        unroll<NT>([&](auto j) {
+        unroll<NF>([&](auto j) {
             constexpr int J = decltype(j)::value;
             if constexpr (J < HALF) read_a(buf, std::integral_constant<int, HALF + J>{});
             multiply(now, Zero{}, j);
             __builtin_amdgcn_sched_barrier(0);
         });
         __syncthreads();                        // every wave's tiles of step t + 1 are there
-        unroll<NT>([&](auto j) {
+        unroll<NF>([&](auto j) {
             constexpr int J = decltype(j)::value;
             if constexpr (J < HALF) read_a(next, j);
-            if constexpr (J == NT / 2 - 1) put(now, after);
-            if constexpr (J == NT / 2) fetch(now, t + 4);
+            if constexpr (J == NF / 2 - 1) put(now, after);
+            if constexpr (J == NF / 2) fetch(now, t + 4);
             multiply(now, Lower{}, j);
             read_b(next, j);
             __builtin_amdgcn_sched_barrier(0);
@@ -235,7 +272,7 @@ __device__ __forceinline__ void product_tile(const Mx4View &a, const Mx4View &b,
         put(One{}, 1);
         fetch(One{}, 3);
         __syncthreads();
-        unroll<NT>([&](auto j) { read_b(0, j); });
+        unroll<NF>([&](auto j) { read_b(0, j); });
         unroll<HALF>([&](auto i) { read_a(0, i); });
         int t = 0;
         for (; t + 1 < steps; t += 2) {
@@ -245,15 +282,14 @@ __device__ __forceinline__ void product_tile(const Mx4View &a, const Mx4View &b,
         if constexpr (ODD) step(Zero{}, t);
     }
 
-    const int64_t m0 = m_tile * 16 + wm * MT * 16 + (lane & 15);
+    const int64_t m0 = m_tile * 16 + wm * MT * 16 + (lane & 31);
     const int64_t n0 = n_tile * 16 + wn * NT * 16;
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int64_t m = m0 + i * 16;
+    for (int i = 0; i < MF; ++i) {
+        const int64_t m = m0 + i * 32;
 #pragma unroll
-        for (int j = 0; j < NT; j += 2)
-            store_pair<GT>(out + m * ld, n0 + j * 16, b.rows, m < a.rows, acc[i][j], acc[i][j + 1],
-                           lane);
+        for (int j = 0; j < NF; ++j)
+            store_row<GT>(out + m * ld, n0 + j * 32, b.rows, m < a.rows, acc[i][j], block);
         __builtin_amdgcn_sched_barrier(0);
     }
 }
@@ -337,12 +373,17 @@ hipError_t launch_mx4_product(const Mx4View &a, const Mx4View &b, void *out, int
 {
     if (a.rows == 0 || b.rows == 0) return hipSuccess;
     if (a.rows <= kFewRows) return launch_mx4_few(a, b, out, gt, ld, st);
+    // Large tiles need less of memory and LDS per product: they pay from two thirds of
+    // a round of the GPU on; then 128 x 128 while that occupies half of it, then
+    // 128 x 64.  Measured both sides (us): 6400 x 1600 by 8192, 175 large tiles, 58 / 63 by
+    // 128 x 128; 2047 x 4096 by 1024, 128 large tiles, 15.3 / 12.6; 300 x 6400 by 1600, 150
+    // tiles of 128 x 128, 8.5 / 9.8 by 128 x 64; 2047 x 1024 by 4096, 128 of them, 15.3 / 13.3.
     const auto count = [&](int64_t m, int64_t n) {
         return (a.rows + m - 1) / m * ((b.rows + n - 1) / n);
     };
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
-        if (count(256, 256) >= 224) return launch_large<GT>(a, b, out, ld, st);
+        if (count(256, 256) >= 168) return launch_large<GT>(a, b, out, ld, st);
         if (count(128, 128) >= 144) return launch_tiles<GT, 4, 4, 2>(a, b, out, ld, st);
         return launch_tiles<GT, 4, 4, 1>(a, b, out, ld, st);
     });

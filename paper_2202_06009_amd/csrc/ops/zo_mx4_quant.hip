@@ -80,6 +80,7 @@ __global__ __launch_bounds__(256) void k_mx4_quantize(const typename Elem<GT>::T
 #pragma unroll
     for (int h = 0; h < TR / 64; ++h) {
         const int64_t row0 = rt * TR + h * 64;
+        if (!COLS && row0 >= rows) break;
         uint32_t w[4][D];
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
