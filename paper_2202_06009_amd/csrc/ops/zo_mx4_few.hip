@@ -6,8 +6,8 @@
 // KS waves of a group share them, each a run of the tiles, and their sums are
 // joined in a fixed order through shared memory.
 //
-// Up to 16 rows of activations that fit shared memory are quantised by every
-// workgroup for itself (FUSED): no second kernel, nothing written and read back.
+// Up to 16 rows of activations, where they are few tiles (few_fused), are quantised by
+// every workgroup for itself (FUSED): no second kernel, nothing written and read back.
 #include "zo_mx4_device.h"
 
 namespace zo {
@@ -34,30 +34,30 @@ __device__ __forceinline__ void store_few(typename Elem<GT>::T *p, const f32x4 &
     }
 }
 
-// The 16 x (128 kt) activations in the operand's order: codes[t][lane], and a
-// scale byte for each.  One block of 32 per thread and turn; rows and columns that
-// are not there are zeros.
+// The rows x (128 kt) activations in the operand's order: codes[t][lane], and a
+// scale byte for each.  One block of 32 per thread and turn; columns that are not there
+// are zeros, rows that are not there stay what they were: they reach no result.
 template <int GX>
-__device__ __forceinline__ void quantize_rows(const typename Elem<GX>::T *x, int64_t rows,
+__device__ __forceinline__ void quantize_rows(const typename Elem<GX>::T *x, int rows,
                                               int64_t cols, int64_t ldx, int kt, u32x4 *codes,
                                               uint8_t *scales)
 {
     constexpr int V = Elem<GX>::kVec, D = 32 / V;      // accesses of a block
-    for (int i = threadIdx.x; i < kt * 64; i += kWaves * 64) {
-        const int r = i & 15;
-        const int64_t col = (int64_t)(i >> 4) * 32;
+#pragma unroll 2
+    for (int b = threadIdx.x; b < kt * 4 * rows; b += kWaves * 64) {
+        const int r = b % rows, k = b / rows, i = k * 16 + r;   // i = tile * 64 + lane
+        const int64_t col = (int64_t)k * 32;
         u32x4 w[D];
         uint32_t a = 0;
 #pragma unroll
         for (int d = 0; d < D; ++d) {
-            w[d] = u32x4{0, 0, 0, 0};
-            if (r < rows) w[d] = load16<GX>(x + r * ldx + col + d * V, cols - col - d * V);
+            w[d] = load16<GX>(x + r * ldx + col + d * V, cols - col - d * V);
 #pragma unroll
             for (int q = 0; q < 4; ++q) a = mag<GX>(a, w[d][q]);
         }
         if constexpr (GX != GT_F32) a = max(a & 0xFFFFu, a >> 16);
-        const uint32_t b = scale_byte<GX>(a);
-        const float s = __uint_as_float(b << 23);
+        const uint32_t e = scale_byte<GX>(a);
+        const float s = __uint_as_float(e << 23);
         u32x4 c;
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
@@ -73,10 +73,10 @@ __device__ __forceinline__ void quantize_rows(const typename Elem<GX>::T *x, int
                 o = convert2<GX, 2>(o, w[d][2], 0, s);
                 o = convert2<GX, 3>(o, w[d][3], 0, s);
             }
-            c[d] = b == 255 ? 0 : o;
+            c[d] = e == 255 ? 0 : o;
         }
-        codes[i] = c;                                  // i = tile * 64 + lane
-        scales[i] = (uint8_t)b;
+        codes[i] = c;
+        scales[i] = (uint8_t)e;
     }
 }
 
@@ -114,7 +114,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_mx4_few(
     };
     fetch(from);                         // in flight while x is quantised
     if constexpr (FUSED) {
-        quantize_rows<GX>(x, a.rows, a.cols, ldx, kt, codes, scales);
+        quantize_rows<GX>(x, (int)a.rows, a.cols, ldx, kt, codes, scales);
         __syncthreads();
     }
     f32x4 acc[MB] = {};
@@ -209,9 +209,15 @@ hipError_t launch_mx4_few(const Mx4View &a, const Mx4View &b, void *out, int gt,
     });
 }
 
+// Every workgroup quantises all of x, so with many tile rows a kernel of its own is
+// faster.  Measured, one kernel / two, us (rows x matrix; tile rows): 1 x 1600 x 6400 (50)
+// 5.9 / 8.6; 16 x 50257 x 1600 (208) 12.2 / 14.3; 8 x 1600 x 6400 (400) 6.4 / 8.4;
+// 8 x 6400 x 6400 (400) 12.0 / 10.2; 16 x 1600 x 6400 (800) 9.8 / 8.5; 16 x 6400 x 6400
+// (800) 17.6 / 10.6.
 bool few_fused(int64_t rows, int64_t cols)
 {
-    return rows <= 16 && (cols + 127) / 128 <= kFusedTiles;
+    const int64_t kt = (cols + 127) / 128;
+    return rows <= 16 && kt <= kFusedTiles && rows * kt <= 400;
 }
 
 hipError_t launch_mx4_few_fused(const void *x, int gx, int64_t rows, int64_t cols, int64_t ldx,

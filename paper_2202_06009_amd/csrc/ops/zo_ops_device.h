@@ -17,7 +17,6 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // The same on any element boundary: one access each, the hardware splits it.
 typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
-typedef uint32_t u32_a2 __attribute__((aligned(2)));
 
 template <int GT>
 struct Elem {
