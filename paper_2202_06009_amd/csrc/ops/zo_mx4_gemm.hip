@@ -27,53 +27,66 @@ __device__ __forceinline__ void unroll(F &&f)
     }
 }
 
-// The 32 columns from n on of a row of results.  16-bit results: the wave's halves
-// swap runs of four, so that a lane holds 8 consecutive columns.
-template <int GT>
-__device__ __forceinline__ void store_row(typename Elem<GT>::T *row, int64_t n, int64_t cols,
-                                          bool inside, const f32x16 &v, int half)
+// 32 rows of a wave's results, NF fragments of 32 columns, through this wave's part of
+// shared memory (no other wave's business), so that a store writes whole runs of 128 or 256
+// bytes: 16-byte chunk c of row r is kept at c ^ (r % 8).  16-bit results: the wave's
+// halves swap runs of four, so that a lane holds 8 consecutive columns.  rows, cols: how
+// many of them are there; STREAM: past the caches (see streamed).  Straight from the
+// registers, 32 bytes of each row: 8192 x 6400 by 128 31 us in 16 bits, 60 in 32; so 27 and 46.
+template <int GT, bool STREAM, int NF>
+__device__ __forceinline__ void store_rows(typename Elem<GT>::T *out, int64_t ld, int64_t rows,
+                                           int64_t cols, const f32x16 (&v)[NF], u32x4 *mine)
 {
-    if constexpr (GT == GT_F32) {
+    constexpr int V = Elem<GT>::kVec, C = 32 * NF / V;     // 16-byte chunks of a row
+    const int lane = threadIdx.x & 63, r = lane & 31, half = lane >> 5;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int64_t at = n + q * 8 + half * 4, nv = cols - at;
-            if (!inside) continue;
-            const u32x4 w = {__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]),
-                             __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3])};
-            if (nv >= 4) {
-                *reinterpret_cast<u32x4_a2 *>(row + at) = w;
-            } else {
-                for (int e = 0; e < 4; ++e)
-                    if (e < nv) row[at + e] = w[e];
-            }
-        }
-    } else {
+    for (int j = 0; j < NF; ++j) {
+        if constexpr (GT == GT_F32) {
 #pragma unroll
-        for (int q = 0; q < 4; q += 2) {
-            u32x4 w;
+            for (int q = 0; q < 4; ++q)
+                mine[r * C + ((j * 8 + q * 2 + half) ^ (r & 7))] =
+                    u32x4{__float_as_uint(v[j][4 * q]), __float_as_uint(v[j][4 * q + 1]),
+                          __float_as_uint(v[j][4 * q + 2]), __float_as_uint(v[j][4 * q + 3])};
+        } else {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint32_t x = (uint32_t)narrow<GT>(v[4 * q + 2 * h]) |
-                                   (uint32_t)narrow<GT>(v[4 * q + 2 * h + 1]) << 16;
-                const uint32_t y = (uint32_t)narrow<GT>(v[4 * q + 4 + 2 * h]) |
-                                   (uint32_t)narrow<GT>(v[4 * q + 5 + 2 * h]) << 16;
-                const auto s = __builtin_amdgcn_permlane32_swap(x, y, false, false);
-                w[h] = s[0];
-                w[2 + h] = s[1];
-            }
-            const int64_t at = n + (q + half) * 8, nv = cols - at;
-            if (!inside) continue;
-            if (nv >= 8) {
-                *reinterpret_cast<u32x4_a2 *>(row + at) = w;
-            } else {
-                for (int e = 0; e < 8; ++e) {
-                    if (e >= nv) break;
-                    const uint32_t d = e < 2 ? w[0] : e < 4 ? w[1] : e < 6 ? w[2] : w[3];
-                    row[at + e] = (uint16_t)(d >> (16 * (e & 1)));
+            for (int q = 0; q < 4; q += 2) {
+                u32x4 w;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t x = (uint32_t)narrow<GT>(v[j][4 * q + 2 * h]) |
+                                       (uint32_t)narrow<GT>(v[j][4 * q + 2 * h + 1]) << 16;
+                    const uint32_t y = (uint32_t)narrow<GT>(v[j][4 * q + 4 + 2 * h]) |
+                                       (uint32_t)narrow<GT>(v[j][4 * q + 5 + 2 * h]) << 16;
+                    const auto s = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+                    w[h] = s[0];
+                    w[2 + h] = s[1];
                 }
+                mine[r * C + ((j * 4 + q + half) ^ (r & 7))] = w;
             }
         }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int i = 0; i < C / 2; ++i) {
+        const int row = i * (64 / C) + lane / C, c = lane % C;
+        const u32x4 w = mine[row * C + (c ^ (row & 7))];
+        typename Elem<GT>::T *to = out + row * ld + c * V;
+        const int64_t nv = row < rows ? cols - c * V : 0;
+        if (nv >= V) {
+            u32x4_a2 *const p = reinterpret_cast<u32x4_a2 *>(to);
+            if constexpr (STREAM)
+                __builtin_nontemporal_store(w, p);
+            else
+                *p = w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (e < nv)
+                    to[e] = (typename Elem<GT>::T)(GT == GT_F32 ? w[e & 3]
+                                                                : w[e / 2] >> (16 * (e & 1)));
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
 // The workgroup's tile of the output.  Workgroups go to the 8 XCDs in turn, each
@@ -128,8 +141,8 @@ __device__ __forceinline__ const uint8_t *scales_at(const Mx4View &x, int64_t gr
 // of loads are in flight, about what the memory's latency takes.
 // ODD: an odd number of steps (the register sets go round by twos).
 //
-// Measured: 16384 x 16384 by 8192 1.13 ms (3.8 PFLOP/s), 8192 x 6400 by 1600 66 us, 8192 x 1600
-// by 6400 53 us.  Bound: copies of the kernel that leave work out (on the 16 x 16 x 128
+// Measured: 16384 x 16384 by 8192 1.13 ms (3.8 PFLOP/s), 8192 x 6400 by 1600 68 us, 8192 x 1600
+// by 6400 55 us.  Bound: copies of the kernel that leave work out (on the 16 x 16 x 128
 // form) took 0.79 ms of 1.12 without any operand traffic, 0.85 without the loads and
 // the writes to shared memory, 1.02 without the reads from it: the loads (32 KiB a
 // step through the L1, about 30 bytes a clock) take the most, the matrix pipe next.
@@ -137,7 +150,7 @@ __device__ __forceinline__ const uint8_t *scales_at(const Mx4View &x, int64_t gr
 // in flight (1.5 ms); workgroups of 128 x 256, two a CU, spill (1.8 ms).
 //
 // The outputs begin at row tile m_tile and column tile n_tile (of 16).
-template <int GT, int MT, int NT, int WN, bool ODD>
+template <int GT, int MT, int NT, int WN, bool ODD, bool STREAM>
 __device__ __forceinline__ void product_tile(const Mx4View &a, const Mx4View &b,
                                              typename Elem<GT>::T *__restrict__ out, int64_t ld,
                                              int64_t m_tile, int64_t n_tile, u32x4 *lds)
@@ -282,27 +295,26 @@ __device__ __forceinline__ void product_tile(const Mx4View &a, const Mx4View &b,
         if constexpr (ODD) step(Zero{}, t);
     }
 
-    const int64_t m0 = m_tile * 16 + wm * MT * 16 + (lane & 31);
-    const int64_t n0 = n_tile * 16 + wn * NT * 16;
+    __syncthreads();                            // every wave has read its last operands
+    static_assert(3 * CHUNKS >= WAVES * 2 * NT, "room for 32 binary32 rows of every wave");
+    const int64_t m0 = m_tile * 16 + wm * MT * 16, n0 = n_tile * 16 + wn * NT * 16;
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
-        const int64_t m = m0 + i * 32;
-#pragma unroll
-        for (int j = 0; j < NF; ++j)
-            store_row<GT>(out + m * ld, n0 + j * 32, b.rows, m < a.rows, acc[i][j], block);
+        store_rows<GT, STREAM>(out + (m0 + i * 32) * ld + n0, ld, a.rows - m0 - i * 32,
+                               b.rows - n0, acc[i], lds + wave * (NT * 4 * 32));
         __builtin_amdgcn_sched_barrier(0);
     }
 }
 
 // One tile a workgroup.
-template <int GT, int MT, int NT, int WN, bool ODD>
+template <int GT, int MT, int NT, int WN, bool ODD, bool STREAM>
 __global__ __launch_bounds__(128 * WN, 2) void k_mx4_product(
     Mx4View a, Mx4View b, typename Elem<GT>::T *__restrict__ out, int64_t ld, uint32_t m_tiles,
     uint32_t n_tiles)
 {
     extern __shared__ u32x4 lds[];                               // [3][CHUNKS][64]
     const TileIndex tile = tile_index(run_index(blockIdx.x, m_tiles * n_tiles), m_tiles, n_tiles);
-    product_tile<GT, MT, NT, WN, ODD>(a, b, out, ld, (int64_t)tile.m * 2 * MT,
+    product_tile<GT, MT, NT, WN, ODD, STREAM>(a, b, out, ld, (int64_t)tile.m * 2 * MT,
                                       (int64_t)tile.n * WN * NT, lds);
 }
 
@@ -316,14 +328,26 @@ __global__ __launch_bounds__(512, 2) void k_mx4_product_large(
     extern __shared__ u32x4 lds[];
     if (blockIdx.x < whole) {
         const TileIndex tile = tile_index(run_index(blockIdx.x, whole), m_tiles, n_tiles);
-        product_tile<GT, 8, 4, 4, ODD>(a, b, out, ld, (int64_t)tile.m * 16, (int64_t)tile.n * 16,
-                                       lds);
+        product_tile<GT, 8, 4, 4, ODD, false>(a, b, out, ld, (int64_t)tile.m * 16,
+                                              (int64_t)tile.n * 16, lds);
     } else {
         const uint32_t half = blockIdx.x - whole;
         const TileIndex tile = tile_index(whole + half / 2, m_tiles, n_tiles);
-        product_tile<GT, 4, 4, 4, ODD>(a, b, out, ld, (int64_t)tile.m * 16 + half % 2 * 8,
+        product_tile<GT, 4, 4, 4, ODD, false>(a, b, out, ld, (int64_t)tile.m * 16 + half % 2 * 8,
                                        (int64_t)tile.n * 16, lds);
     }
+}
+
+// Whether results are stored past the caches: where rows begin on lines of 128 bytes.
+// The small tiles' products are short, and the lines they leave in the L2 are written at
+// the end: 2047 x 4096 by 512 8.2 us against 9.6.  Rows off the lines would be written in
+// parts: 4096 x 4100 by 512 23.6 us against 19.6.  The large tiles gain nothing
+// (8192 x 6400 by 1600 67.2 against 64.8).
+template <int GT>
+static bool streamed(const void *out, int64_t ld)
+{
+    const uint64_t row = (uint64_t)ld * sizeof(typename Elem<GT>::T);
+    return ((reinterpret_cast<uintptr_t>(out) | row) & 127) == 0;
 }
 
 // Shared memory beyond 64 KiB has to be asked for.
@@ -333,7 +357,7 @@ static hipError_t allow_lds(const void *kernel, uint32_t lds)
     return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
 }
 
-template <int GT, int MT, int NT, int WN>
+template <int GT, int MT, int NT, int WN, bool STREAM>
 static hipError_t launch_tiles(const Mx4View &a, const Mx4View &b, void *out, int64_t ld,
                                hipStream_t st)
 {
@@ -341,8 +365,8 @@ static hipError_t launch_tiles(const Mx4View &a, const Mx4View &b, void *out, in
     const int64_t nt = (b.rows + 16 * WN * NT - 1) / (16 * WN * NT);
     const int64_t mt = (a.rows + 32 * MT - 1) / (32 * MT), tiles = mt * nt;
     if (tiles > INT32_MAX || a.kt > INT32_MAX) return hipErrorInvalidValue;
-    const auto kernel =
-        a.kt % 2 ? k_mx4_product<GT, MT, NT, WN, true> : k_mx4_product<GT, MT, NT, WN, false>;
+    const auto kernel = a.kt % 2 ? k_mx4_product<GT, MT, NT, WN, true, STREAM>
+                                 : k_mx4_product<GT, MT, NT, WN, false, STREAM>;
     const hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), lds);
     if (e != hipSuccess) return e;
     kernel<<<dim3((uint32_t)tiles), 128 * WN, lds, st>>>(
@@ -374,18 +398,30 @@ hipError_t launch_mx4_product(const Mx4View &a, const Mx4View &b, void *out, int
     if (a.rows == 0 || b.rows == 0) return hipSuccess;
     if (a.rows <= kFewRows) return launch_mx4_few(a, b, out, gt, ld, st);
     // Large tiles need less of memory and LDS per product: they pay from two thirds of
-    // a round of the GPU on; then 128 x 128 while that occupies half of it, then
-    // 128 x 64.  Measured both sides (us): 6400 x 1600 by 8192, 175 large tiles, 58 / 63 by
-    // 128 x 128; 2047 x 4096 by 1024, 128 large tiles, 15.3 / 12.6; 300 x 6400 by 1600, 150
-    // tiles of 128 x 128, 8.5 / 9.8 by 128 x 64; 2047 x 1024 by 4096, 128 of them, 15.3 / 13.3.
+    // a round of the GPU on, if the steps are many for the time that a workgroup, alone
+    // on its CU, takes to write its results; then 128 x 128 while that occupies half of the
+    // GPU, then 128 x 64.  Measured both sides, us, large / 128 x 128:
+    //   16 bits: 8192 x 6400 by 1600 67.7 / 70.2, by 800 47.5 / 44.1, by 128 28.1 / 24.1;
+    //   4096 x 4096 by 1024 17.4 / 17.9; 8192 x 1600 by 6400 55 / 69
+    //   32 bits: 8192 x 6400 by 2560 106 / 104, by 1600 81 / 76, by 800 61 / 50; 4096 x 4096
+    //   by 2048 29.3 / 30.5; 8192 x 1600 by 6400 56 / 70
+    //   32 bits, rows off the lines: 8192 x 6402 by 800 74 / 87; 4096 x 50257 by 256 243 / 215
+    // 2047 x 4096 by 1024, 128 large tiles: 15.3 / 12.6 on an earlier form.  128 x 128 /
+    // 128 x 64, on the same: 300 x 6400 by 1600, 150 tiles of 128 x 128, 8.5 / 9.8;
+    // 2047 x 1024 by 4096, 128 of them, 15.3 / 13.3.
     const auto count = [&](int64_t m, int64_t n) {
         return (a.rows + m - 1) / m * ((b.rows + n - 1) / n);
     };
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
-        if (count(256, 256) >= 168) return launch_large<GT>(a, b, out, ld, st);
-        if (count(128, 128) >= 144) return launch_tiles<GT, 4, 4, 2>(a, b, out, ld, st);
-        return launch_tiles<GT, 4, 4, 1>(a, b, out, ld, st);
+        const bool stream = streamed<GT>(out, ld);
+        if (count(256, 256) >= 168 && a.kt >= (GT != GT_F32 ? 8 : stream ? 20 : 3))
+            return launch_large<GT>(a, b, out, ld, st);
+        if (count(128, 128) >= 144)
+            return stream ? launch_tiles<GT, 4, 4, 2, true>(a, b, out, ld, st)
+                          : launch_tiles<GT, 4, 4, 2, false>(a, b, out, ld, st);
+        return stream ? launch_tiles<GT, 4, 4, 1, true>(a, b, out, ld, st)
+                      : launch_tiles<GT, 4, 4, 1, false>(a, b, out, ld, st);
     });
 }
 

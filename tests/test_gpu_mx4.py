@@ -168,7 +168,9 @@ def test_product_and_linear(torch, mnk):
 
 
 @pytest.mark.parametrize("m,n,k", [(2300, 7300, 200), (4090, 4100, 60), (2050, 8200, 300),
-                                   (2048, 17900, 60), (2000, 16300, 130), (6333, 1601, 1200)])
+                                   (2048, 17900, 60), (2000, 16300, 130), (6333, 1601, 1200),
+                                   (2500, 7296, 1300), (4200, 4303, 1020),
+                                   (3000, 6208, 2600)])
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_product_of_many_tiles(torch, m, n, k, dtype):
     """More tiles than the GPU has CUs, whole rounds of them and a rest; compared on
