@@ -223,63 +223,70 @@ __device__ __forceinline__ void put16(typename Elem<GT>::T *p, const u32x4 &w, i
         store16<GT>(p, w, nv);
 }
 
-// 16 lanes per row of a 128-column tile, 8 elements each, four rows a thread.  The
-// conversion to binary32 is exact; its upper half is the bfloat16.
+// 16 lanes per row of a 128-column tile and 16 bytes of results at a time (8 elements, or
+// 4 of each half of the tile), so that a store writes 256 contiguous bytes of a row;
+// four rows a thread.  The conversion to binary32 is exact; its upper half is the bfloat16.
 //
-// NT: nontemporal stores, for rows on 16-byte boundaries (whole lines are written
-// once: 16384 x 8192 bfloat16 66 -> 49 us, 8192 x 1600 6.4 -> 5.4 us); off them a
-// store touches two lines and both are completed later (8191 x 4097 binary16: 17 us,
-// 29 us nontemporal).
+// NT: nontemporal stores, for rows on lines of 128 bytes, which are then written once:
+// 16384 x 8192 bfloat16 66 -> 49 us, 8191 x 4096 binary32 27.5 -> 24.6 us (7.0 TB/s).  Off
+// the lines a store touches parts of some: 8191 x 4104 binary16 16 us, 30 us nontemporal;
+// 8191 x 4097 17.6 us.  Eight elements of a lane side by side, in binary32 two stores of
+// every other 16 bytes, took 72 us for 8191 x 4096.
 template <int GT, bool NT>
 __global__ __launch_bounds__(256) void k_mx4_dequantize(Mx4View q,
                                                         typename Elem<GT>::T *__restrict__ out,
                                                         int64_t ld, uint32_t col_tiles)
 {
+    constexpr int V = Elem<GT>::kVec, G = 8 / V, PER = 32 / V;   // lanes of a block of 32
+    using Codes = std::conditional_t<GT == GT_F32, uint16_t, uint32_t>;
     const int tid = threadIdx.x, i = tid & 15, rr = tid >> 4;
     const int64_t rt = blockIdx.x / col_tiles, ct = blockIdx.x % col_tiles;
-    const int64_t col = ct * 128 + i * 8, nv = q.cols - col;
-    if (nv <= 0) return;
-    const uint32_t bytes = *reinterpret_cast<const uint32_t *>(
-        q.scales + ((rt * q.kt + ct) * 64 + (i >> 2) * 16 + rr) * 4);
-    uint32_t c[4];
+    const int64_t col = ct * 128 + i * V;
+    uint32_t bytes[G], c[G][4];
 #pragma unroll
-    for (int p = 0; p < 4; ++p)      // rows beyond the matrix are stored as well
-        c[p] = *reinterpret_cast<const uint32_t *>(
-            q.codes + ((rt * 4 + p) * q.kt + ct) * 1024 + ((i >> 2) * 16 + rr) * 16 + (i & 3) * 4);
+    for (int g = 0; g < G; ++g) {
+        const int at = (g * 2 + i / PER) * 16 + rr;              // block and row
+        bytes[g] =
+            *reinterpret_cast<const uint32_t *>(q.scales + ((rt * q.kt + ct) * 64 + at) * 4);
+#pragma unroll
+        for (int p = 0; p < 4; ++p)      // rows beyond the matrix are stored as well
+            c[g][p] = *reinterpret_cast<const Codes *>(
+                q.codes + ((rt * 4 + p) * q.kt + ct) * 1024 + at * 16 + i % PER * (V / 2));
+    }
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const int64_t row = rt * 64 + p * 16 + rr;
         if (row >= q.rows) return;
-        const uint32_t b = bytes >> (8 * p) & 255u;
-        const float s = __uint_as_float(b << 23);
-        typedef float f32x2 __attribute__((ext_vector_type(2)));
-        const f32x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[p], s, 0),
-                            __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[p], s, 1),
-                            __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[p], s, 2),
-                            __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[p], s, 3)};
-        constexpr float kNan = __builtin_nanf("");
-        typename Elem<GT>::T *o = out + row * ld + col;
-        if constexpr (GT == GT_F32) {
-            u32x4 lo, hi;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                lo[j] = __float_as_uint(b == 255 ? kNan : v[j >> 1][j & 1]);
-                hi[j] = __float_as_uint(b == 255 ? kNan : v[2 + (j >> 1)][j & 1]);
-            }
-            put16<GT, NT>(o, lo, nv);
-            if (nv > 4) put16<GT, NT>(o + 4, hi, nv - 4);
-        } else {
+        for (int g = 0; g < G; ++g) {
+            const int64_t nv = q.cols - col - g * 64;
+            if (nv <= 0) break;
+            const uint32_t b = bytes[g] >> (8 * p) & 255u;
+            const float s = __uint_as_float(b << 23);
+            typedef float f32x2 __attribute__((ext_vector_type(2)));
             u32x4 w;
+            if constexpr (GT == GT_F32) {
+                const f32x2 v[2] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[g][p], s, 0),
+                                    __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[g][p], s, 1)};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (GT == GT_BF16)
-                    w[j] = __builtin_amdgcn_perm(__float_as_uint(v[j][1]), __float_as_uint(v[j][0]),
-                                                 0x07060302u);
-                else
-                    w[j] = (uint32_t)narrow<GT>(v[j][0]) | (uint32_t)narrow<GT>(v[j][1]) << 16;
-                if (b == 255) w[j] = GT == GT_BF16 ? 0x7FC07FC0u : 0x7E007E00u;
+                for (int j = 0; j < 4; ++j)
+                    w[j] = b == 255 ? 0x7FC00000u : __float_as_uint(v[j >> 1][j & 1]);
+            } else {
+                const f32x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[g][p], s, 0),
+                                    __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[g][p], s, 1),
+                                    __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[g][p], s, 2),
+                                    __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[g][p], s, 3)};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if constexpr (GT == GT_BF16)
+                        w[j] = __builtin_amdgcn_perm(__float_as_uint(v[j][1]),
+                                                     __float_as_uint(v[j][0]), 0x07060302u);
+                    else
+                        w[j] = (uint32_t)narrow<GT>(v[j][0]) | (uint32_t)narrow<GT>(v[j][1]) << 16;
+                    if (b == 255) w[j] = GT == GT_BF16 ? 0x7FC07FC0u : 0x7E007E00u;
+                }
             }
-            put16<GT, NT>(o, w, nv);
+            put16<GT, NT>(out + row * ld + col + g * 64, w, nv);
         }
     }
 }
@@ -292,7 +299,7 @@ hipError_t launch_mx4_dequantize(const Mx4View &q, void *out, int gt, int64_t ld
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
         auto *p = static_cast<typename Elem<GT>::T *>(out);
-        if ((uintptr_t)p % 16 == 0 && ld * sizeof(*p) % 16 == 0)
+        if ((uintptr_t)p % 128 == 0 && ld * sizeof(*p) % 128 == 0)
             k_mx4_dequantize<GT, true><<<dim3((uint32_t)tiles), 256, 0, st>>>(q, p, ld,
                                                                              (uint32_t)q.kt);
         else
