@@ -158,12 +158,15 @@ typedef struct zo_distill {
  *   loss = w (kd_weight tau^2 KL + ce_weight (lse(z) - z[label])),
  *   dz = w (kd_weight tau d + ce_weight (softmax(z) - onehot(label))),
  *     d = q - p on S; outside S d = q, with L q - p_r (q / q_r).
- * A part whose weight is 0 is left out.  Outcomes with p = 0 add 0 to KL; one with p > 0 that the student excludes
- * (logits of -infinity) makes the loss +infinity and leaves the gradient
- * finite, and so does an excluded label.  p_r below 2^-16 counts as 0 where
- * the student excludes everything outside S: it is no more than the rounding
- * of L.  A student row of only -infinity has q = 0.  Without L, a row whose used
- * slots hold no teacher's logit above -infinity has no KL part.
+ * A part whose weight is 0 is left out.  Outcomes with p = 0 add 0 to KL; one
+ * with p > 0 that the student excludes (logits of -infinity, and those whose
+ * distance from the row's largest, over tau, passes binary32) makes the loss
+ * +infinity and leaves the gradient finite, and so does an excluded label.
+ * p_r below 2^-16 counts as 0 where the student excludes everything outside S or
+ * its largest logit there has less than 2^-32768 of the row's largest one's
+ * probability (masks of -1e9 or of a type's lowest value): it is no more than
+ * the rounding of L.  A student row of only -infinity has q = 0.  Without L, a
+ * row whose used slots hold no teacher's logit above -infinity has no KL part.
  */
 int zo_distill_loss(const zo_distill *args, hipStream_t stream);
 

@@ -25,8 +25,10 @@ namespace zo {
 constexpr int kMaxTop = 1024;
 
 // What 1 - sum p is known to, its terms being rounded exponentials of numbers
-// around 10: where the student has nothing outside S, less than this is nothing.
-constexpr float kRestRounding = 0x1p-16f;
+// around 10: where the student has nothing outside S, or less than 2^-32768 (masks of
+// -1e9 or a type's lowest value: the logarithm would make the rounding the loss), less
+// than this is nothing.
+constexpr float kRestRounding = 0x1p-16f, kNothing = -32768.0f;
 
 // The base b of a sum whose largest logit is m; 0 for an empty sum.
 template <bool FAR>
@@ -47,6 +49,13 @@ template <bool FAR>
 __device__ __forceinline__ float between(float b, float to, float c)
 {
     return FAR ? (b - to) * c : b - to;
+}
+
+// ln of the same.
+template <bool FAR>
+__device__ __forceinline__ float log_between(float b, float to, float c, float tau)
+{
+    return FAR ? (b - to) / tau : between<FAR>(b, to, c) * kLn2;
 }
 
 // How the label's softmax (tau = 1) follows from e: as e (and where no labels are
@@ -218,7 +227,7 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, const Row<TH> &
     t.pr = 0.0f;
     if (R.tail) {
         t.pr = fmaxf(0.0f, 1.0f - psum);
-        if (t.no_rest && t.pr < kRestRounding) t.pr = 0.0f;
+        if ((t.no_rest || log_to_all < kNothing) && t.pr < kRestRounding) t.pr = 0.0f;
     }
     const float log_p = R.tail ? 0.0f : logf(psum), log_all = logf(t.s_all);
     // p log(p / q) - p + q for each outcome: what is added sums to 0 over all
@@ -248,8 +257,17 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, const Row<TH> &
         kl = group_get<OpSum, NW>(s.red[9]);
         qsum = group_get<OpSum, NW>(s.red[10]);
         if (R.tail) {
+            // log(pr / qr) from the logarithms where qr is near the end of binary32 or past it
             const float qr = t.s_out * t.share;
-            kl += t.pr > 0.0f ? (qr > 0.0f ? t.pr * logf(t.pr / qr) - t.pr + qr : INFINITY) : qr;
+            if (t.pr > 0.0f && t.no_rest)
+                kl = INFINITY;
+            else if (t.pr > 0.0f && qr < 0x1p-100f)
+                kl += t.pr * (logf(t.pr) - (log_between<FAR>(t.b_out, t.b_all, c, a.tau) +
+                                            logf(t.s_out / t.s_all))) - t.pr + qr;
+            else if (t.pr > 0.0f)
+                kl += t.pr * logf(t.pr / qr) - t.pr + qr;
+            else
+                kl += qr;
             kl += fmaxf(0.0f, psum - 1.0f);
         } else if (!t.none) {
             kl += 1.0f - qsum;

@@ -1,0 +1,59 @@
+"""The distillation loss where logits lie far from each other, under masks and near the
+ends of the type, against the 64-bit oracle within limits of each row's own."""
+import numpy as np
+import pytest
+
+import logit_bounds as lb
+
+pytestmark = pytest.mark.gpu
+
+LOWEST = {"float32": -lb.FLT_MAX, "float16": -65504.0, "bfloat16": -float.fromhex("0x1.fep127")}
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return torch
+
+
+def _check(torch, dtype, z, vals, cols, *, inplace=False, **kw):
+    import paper_2202_06009_amd as zo
+
+    def dev(a, dt):
+        return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).to(dt).cuda()
+    x = torch.from_numpy(z).to(getattr(torch, dtype)).cuda()
+    z = x.double().cpu().numpy()
+    loss = torch.full((len(z),), 7.0, device="cuda")
+    dz = x if inplace else torch.full_like(x, 7.0)
+    f32, i32 = torch.float32, torch.int32
+    zo.zo_distill_loss(x, dev(vals, f32), dev(cols, i32), loss, dz, tau=kw.get("tau", 1.0),
+                       teacher_lse=dev(kw.get("lse"), f32), labels=dev(kw.get("labels"), i32),
+                       kd_weight=kw.get("kd", 1.0), ce_weight=kw.get("ce", 0.0),
+                       row_weight=dev(kw.get("weight"), f32))
+    loss, dz = loss.double().cpu().numpy(), dz.double().cpu().numpy()
+    with np.errstate(all="ignore"):
+        want, want_dz, lim, lim_dz = lb.distill(z, vals, cols, dtype, **kw)
+        off, off_dz = np.abs(loss - want), np.abs(dz - want_dz)
+    bad = ~((loss == want) | (off <= lim))
+    assert not bad.any(), (np.flatnonzero(bad), loss[bad], want[bad], lim[bad])
+    bad = ~(off_dz <= lim_dz)
+    at = np.argwhere(bad)[:4]
+    assert not bad.any(), (at, [(dz[i, j], want_dz[i, j], lim_dz[i, j]) for i, j in at])
+
+
+# rows in registers, and rows that are read twice
+VOCABS = [40, 3001, 50257, 70001, 140001]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("vocab", VOCABS)
+@pytest.mark.parametrize("tau", [0.5, 1.0, 2.0])
+def test_rest_far_below(torch, vocab, tau, dtype):
+    """A student that holds all outside S far below S, but not excluded: the loss is finite,
+    and where the teacher has nothing there either, its rounding is not made a loss."""
+    masks = [-100.0, -1e4, max(-1e9, LOWEST[dtype]), LOWEST[dtype]]
+    z, vals, cols, lse, _ = lb.far_rest_rows(vocab, tau, masks, False)
+    _check(torch, dtype, z, vals, cols, tau=tau, lse=lse)
+    _check(torch, dtype, z, vals, cols, tau=tau, lse=lse, kd=0.7, inplace=True)
