@@ -14,10 +14,10 @@
 // sweeps instead of two.
 //
 // c z - b is one fused operation, rounded relative to itself; b's own rounding
-// is common to every term and cancels.  Where c z could overflow (the row's
-// largest logit is near the end of binary32) and in rows that do not fit
-// registers (k_distill_long, two reads), the difference z - b is formed first,
-// b being the largest logit itself (FAR).
+// is common to every term and cancels.  Where that rounding is itself many
+// exponents (the products of the row's largest logits are 2^31 or more) and in rows
+// that do not fit registers (k_distill_long, two reads), the difference z - b is
+// formed first, b being the largest logit itself (FAR).
 #include "zo_ops_device.h"
 
 namespace zo {
@@ -507,10 +507,12 @@ __global__ __launch_bounds__(TH, 4) void k_distill(zo_distill a)
     m_out = group_get<OpMax, NW>(s.red[0]);
     m_in = group_get<OpMax, NW>(s.red[1]);
     um = group_get<OpMax, NW>(s.red[2]);
-    // the products of both largest logits (-infinity: none) with both factors are finite
+    // below 2^31, the products of both largest logits (-infinity: none) with both factors
+    // are rounded by at most 64, so that an e of the largest is within 2^-64 to 2^64, and
+    // its square at tau = 2, where c is half as large, as well
     const float size = fmaxf(m_out == -INFINITY ? 0.0f : fabsf(m_out),
                              m_in == -INFINITY ? 0.0f : fabsf(m_in));
-    if (!(size * fmaxf(R.c, kLog2e) < 0x1p126f)) {
+    if (!(size * fmaxf(R.c, kLog2e) < 0x1p31f)) {
         far_row<GT, F, TH>(a, R, s, bits, z, dz);
         return;
     }

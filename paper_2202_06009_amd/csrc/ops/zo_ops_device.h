@@ -263,8 +263,9 @@ __device__ __forceinline__ void repack(u32x4 &w)
 
 // Where a sum of exponentials has its reference: 2^(z c - r) with r the largest
 // z c rounded.  z c - r is one fused operation, rounded relative to itself, and
-// r's own rounding is common to every term, so it cancels.  A largest logit of
-// -infinity gives 0: every term is then 0.
+// r's own rounding is common to every term, so it cancels, while it is small for an
+// exponent (|r| < 2^31: at most 64).  A largest logit of -infinity gives 0: every term
+// is then 0.
 __device__ __forceinline__ float reference(float m, float c)
 {
     return m == -INFINITY ? 0.0f : m * c;

@@ -414,34 +414,33 @@ __global__ __launch_bounds__(TH, TH == 768 ? 6 : 4) void k_top(TopArgs a)
     else
         least = find_bound<TH>(s, (uint32_t)a.top, M, m);
     const float total = group_get<OpSum, NW>(s.red[2]);
-    if (total != total || !(fabsf(r) < 0x1p126f) || unbound) {   // or c z near overflow
-        if (a.lse) lse_row<GT, TH>(a, row, s);
-        select_row<GT, TH>(a, row, s);
-        return;
-    }
-    if (a.lse && tid == 0) a.lse[row] = lse_of(M, total, a.tau, false);
-    // collect
-    const float bound = key_value(least);
-    if (x.has_last(V) && (all || x.last >= bound)) offer<TH>(s, x.last, x.last_column());
+    // from 2^31 on the rounding of r is many exponents
+    const bool plain = total == total && fabsf(r) < 0x1p31f;
+    bool counted = total != total || unbound;
+    if (a.lse && plain && tid == 0) a.lse[row] = lse_of(M, total, a.tau, false);
+    if (!counted) {                                      // collect
+        const float bound = key_value(least);
+        if (x.has_last(V) && (all || x.last >= bound)) offer<TH>(s, x.last, x.last_column());
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        repack<GT>(x.w[v]);
-        if (x.at(v) < x.vecs && (all || max_of<GT>(x.w[v]) >= bound)) {
+        for (int v = 0; v < NV; ++v) {
+            repack<GT>(x.w[v]);
+            if (x.at(v) < x.vecs && (all || max_of<GT>(x.w[v]) >= bound)) {
 #pragma unroll
-            for (int q = 0; q < K; ++q) {
-                const float z = elem_of<GT>(x.w[v], q);
-                if (all || z >= bound) offer<TH>(s, z, x.at(v) * K + q);
+                for (int q = 0; q < K; ++q) {
+                    const float z = elem_of<GT>(x.w[v], q);
+                    if (all || z >= bound) offer<TH>(s, z, x.at(v) * K + q);
+                }
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();
+        counted = s.sel[3] > kRoom;
     }
-    __syncthreads();
-    const uint32_t n = s.sel[3];
-    if (n > kRoom) {
+    if (counted)
         select_row<GT, TH>(a, row, s);
-        return;
-    }
-    sort_out<TH>(a, row, s, (int)n);
+    else
+        sort_out<TH>(a, row, s, (int)s.sel[3]);
+    if (a.lse && !plain) lse_row<GT, TH>(a, row, s);     // the row's registers are free
 }
 
 template <int GT, int TH, int NV>

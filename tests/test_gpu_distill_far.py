@@ -57,3 +57,17 @@ def test_rest_far_below(torch, vocab, tau, dtype):
     z, vals, cols, lse, _ = lb.far_rest_rows(vocab, tau, masks, False)
     _check(torch, dtype, z, vals, cols, tau=tau, lse=lse)
     _check(torch, dtype, z, vals, cols, tau=tau, lse=lse, kd=0.7, inplace=True)
+
+
+@pytest.mark.parametrize("vocab", VOCABS)
+@pytest.mark.parametrize("tau", [1.0, 2.0, 1.5])
+def test_large_logits(torch, vocab, tau):
+    """Rows at values whose products' units in the last place are many exponents."""
+    z, vals, cols, lse, _ = lb.far_rest_rows(vocab, tau, [-1e12, -1e30], False)
+    _check(torch, "float32", z, vals, cols, tau=tau, lse=lse)
+    _check(torch, "bfloat16", z, vals, cols, tau=tau, lse=lse, inplace=True)
+    z, vals, cols, lse, labels = lb.large_rows(vocab, tau)
+    for tail in (False, True):
+        _check(torch, "float32", z, vals, cols, tau=tau, lse=lse if tail else None)
+        _check(torch, "float32", z, vals, cols, tau=tau, lse=lse if tail else None, labels=labels,
+               ce=0.5, inplace=True)

@@ -1,0 +1,66 @@
+"""The top logits' log-sum-exp under masks, at large values and near the ends of the
+type, against the 64-bit oracle within limits of each row's own."""
+import numpy as np
+import pytest
+
+import logit_bounds as lb
+import operators_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+LOWEST = {"float32": -lb.FLT_MAX, "float16": -65504.0, "bfloat16": -float.fromhex("0x1.fep127")}
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return torch
+
+
+def _check(torch, dtype, z, top, tau):
+    import paper_2202_06009_amd as zo
+    x = torch.from_numpy(z).to(getattr(torch, dtype)).cuda()
+    z = x.double().cpu().numpy()
+    rows = len(z)
+    values = torch.full((rows, top), 7.0, device="cuda")
+    columns = torch.full((rows, top), -7, dtype=torch.int32, device="cuda")
+    lse = torch.full((rows,), 7.0, device="cuda")
+    zo.zo_top_logits(x, values, columns, lse, tau=tau)
+    wv, wc, wl = ref.top_logits(z, top, tau)
+    np.testing.assert_array_equal(columns.cpu().numpy(), wc)
+    np.testing.assert_array_equal(values.double().cpu().numpy(), wv)
+    lse, lim = lse.double().cpu().numpy(), lb.lse(z, tau)
+    with np.errstate(invalid="ignore"):
+        bad = ~((lse == wl) | (np.abs(lse - wl) <= lim) | (np.isnan(lse) & np.isnan(wl)))
+    assert not bad.any(), (np.flatnonzero(bad), lse[bad], wl[bad], lim[bad])
+
+
+@pytest.mark.parametrize("vocab", [130, 5000, 50257, 70001, 140001])
+@pytest.mark.parametrize("tau", [1.0, 1.5, 2.0])
+def test_masks(torch, vocab, tau):
+    r = np.random.default_rng(vocab)
+    for dtype in ("float32", "float16", "bfloat16"):
+        z = r.normal(size=(7, vocab)) * 3
+        z[0, ::2] = LOWEST[dtype]
+        z[1] = -np.inf
+        z[2] = -np.inf
+        z[2, vocab // 2:vocab // 2 + 3] = [1.0, 2.0, 1.0]
+        z[3] = LOWEST[dtype]
+        z[3, [3, vocab - 1]] = 0.5
+        z[4] = r.integers(0, 3, vocab)
+        z[5, 11], z[5, 12] = np.inf, np.nan
+        z[6, 10:40] = np.inf
+        for top in (1, 8, 100):
+            _check(torch, dtype, z, top, tau)
+
+
+@pytest.mark.parametrize("vocab", [130, 5000, 50257, 70001])
+@pytest.mark.parametrize("tau", [1.0, 1.5, 2.0])
+def test_large_logits(torch, vocab, tau):
+    """Rows at values whose products' units in the last place are many exponents, and
+    near the ends of binary32."""
+    for z in (lb.large_rows(vocab, tau)[0], lb.extreme_rows(vocab, tau)[0]):
+        for top in (1, 8, 100):
+            _check(torch, "float32", z, top, tau)
