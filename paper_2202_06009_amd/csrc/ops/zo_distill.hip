@@ -58,6 +58,14 @@ __device__ __forceinline__ float log_between(float b, float to, float c, float t
     return FAR ? (b - to) / tau : between<FAR>(b, to, c) * kLn2;
 }
 
+// ln of e about the row's largest logit m, from l, its log2: from the difference itself
+// where its product with log2(e) / tau may have passed binary32 (a label or a slot at the
+// type's lowest value).
+__device__ __forceinline__ float log_above(float z, float m, float tau, float l)
+{
+    return l < -0x1p100f ? (z - m) / tau : l * kLn2;
+}
+
 // How the label's softmax (tau = 1) follows from e: as e (and where no labels are
 // given), as e^2, by an exponential of its own.
 enum LabelForm { kSame, kSquare, kOwn };
@@ -243,7 +251,7 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, const Row<TH> &
         else if (t.none || z == -INFINITY)
             kl = INFINITY;
         else
-            kl += p * (logp - (l * kLn2 - log_all)) - p + q;
+            kl += p * (logp - (log_above(z, m_all, a.tau, l) - log_all)) - p + q;
         qsum += q;
     });
     for (float *x : {&t.b_out, &t.b_all, &t.b_one, &t.s_out, &t.s_all, &t.s_one, &t.share, &t.pr,
@@ -275,8 +283,8 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, const Row<TH> &
         float l = 0.0f;
         if (t.kd) l = a.kd_weight * a.tau * a.tau * kl;
         if (R.y >= 0) {
-            const float lz = above_one<FAR, F>(R.zy, c, t);
-            l += a.ce_weight * (R.zy == -INFINITY ? INFINITY : logf(t.s_one) - lz * kLn2);
+            const float lz = log_above(R.zy, m_all, 1.0f, above_one<FAR, F>(R.zy, c, t));
+            l += a.ce_weight * (R.zy == -INFINITY ? INFINITY : logf(t.s_one) - lz);
         }
         a.loss[R.row] = R.w * l;
     }

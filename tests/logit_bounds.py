@@ -117,8 +117,9 @@ def distill(z, vals, cols, dtype, *, tau=1.0, lse=None, labels=None, kd=1.0, ce=
             grad[out] = q[out] * eq[out]
             if lse is not None:
                 pr = max(0.0, 1.0 - p.sum())
-                r, logr = _softmax(x[out] / tau)
                 m_out = _largest(x[out])              # below the row's largest, or -infinity
+                rest = z[t, out] - (_largest(z[t, out]) if m_out > -np.inf else 0.0)
+                r, logr = _softmax(rest / tau)
                 if -m_out / tau > FAR and pr < 2.0 ** -16:
                     pr = 0.0
                 if pr > 0:
@@ -135,7 +136,7 @@ def distill(z, vals, cols, dtype, *, tau=1.0, lse=None, labels=None, kd=1.0, ce=
                 if m_out > -np.inf and -m_out / tau <= FAR or pr > 0:
                     far = max(-m_out / tau, 0.0) if m_out > -np.inf else 0.0
                     err += err_p * (far + np.log(vocab) + abs(np.log(err_p)) + 2)
-                    of = _exponents(logr, (x[out] - m_out) / tau if m_out > -np.inf else logr)
+                    of = _exponents(logr, rest / tau)
                     grad[out] += r * (err_p + pr * (of + _sum(vocab)))
         row, g = kd * tau * tau * kl, kd * tau * d
         lim, grad = kd * tau * tau * err, kd * tau * grad
@@ -151,6 +152,8 @@ def distill(z, vals, cols, dtype, *, tau=1.0, lse=None, labels=None, kd=1.0, ce=
             if logs[y] > -np.inf:
                 lim += ce * (2 * e1[y] + 8 * E * abs(logs[y]))
         loss[t], dz[t] = w * row, w * g
+        if abs(loss[t]) > FLT_MAX * (1 + E):
+            loss[t] = np.copysign(np.inf, loss[t])
         lim_loss[t] = abs(w) * lim + (16 * E * abs(loss[t]) if np.isfinite(loss[t]) else 0.0)
         grad = abs(w) * grad + 16 * E * np.abs(dz[t])
         lim_dz[t] = grad + HALF_ULP[dtype] * (np.abs(dz[t]) + grad)
