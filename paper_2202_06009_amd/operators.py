@@ -128,6 +128,8 @@ _functions = {}
 def _run(where, dev, stream, args, tensors):
     """Calls the C function on `stream` (the current stream of GPU `dev` when None);
     `tensors` are those that the kernels touch."""
+    if stream is not None and stream.device_index != dev:
+        raise ValueError(f"stream: expected one of GPU {dev}, got one of GPU {stream.device_index}")
     f = _functions.get(where)
     if f is None:
         f = _functions[where] = getattr(lib(), where)
