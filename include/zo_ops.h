@@ -17,6 +17,9 @@
  *   - Element types are ZO_DTYPE_F32, ZO_DTYPE_F16 and ZO_DTYPE_BF16.  Matrices
  *     of these types are row-major with a row stride `ld` in elements
  *     (ld >= columns) and need no alignment beyond their element's.
+ *   - A launch holds fewer than 2^32 threads.  A call on matrices that needs more
+ *     (none below 2^23 tiles of 64 x 128 elements or results does) is ZO_EINVAL;
+ *     logits go into as many launches as their rows take, up to 2^31 - 1 of them.
  *   - Buffers that a call writes may not overlap any other of its buffers,
  *     except where the call says so.
  *   - Sums, softmax statistics and products accumulate in binary32; a result

@@ -577,9 +577,8 @@ static void launch_form(const zo_distill &a, hipStream_t st)
         k_distill<GT, F, 256, 4><<<grid, 256, lds, st>>>(a);
 }
 
-hipError_t launch_distill(const zo_distill &a, hipStream_t st)
+static hipError_t launch_rows(const zo_distill &a, hipStream_t st)
 {
-    if (a.rows == 0) return hipSuccess;
     const int gt = a.dtype == ZO_DTYPE_F16 ? GT_F16 : a.dtype == ZO_DTYPE_BF16 ? GT_BF16 : GT_F32;
     const bool labels = a.labels && a.ce_weight != 0.0f;
     return with_elem_type(gt, [&](auto g) {
@@ -592,6 +591,26 @@ hipError_t launch_distill(const zo_distill &a, hipStream_t st)
             launch_form<GT, kOwn>(a, st);
         return hipGetLastError();
     });
+}
+
+hipError_t launch_distill(const zo_distill &a, hipStream_t st)
+{
+    const int64_t size = a.dtype == ZO_DTYPE_F32 ? 4 : 2;
+    for (int64_t r = 0; r < a.rows; r += kLaunchRows) {
+        zo_distill part = a;
+        part.rows = a.rows - r < kLaunchRows ? a.rows - r : kLaunchRows;
+        part.z = static_cast<const char *>(a.z) + r * a.ldz * size;
+        part.values += r * a.top;
+        part.columns += r * a.top;
+        if (a.teacher_lse) part.teacher_lse += r;
+        if (a.labels) part.labels += r;
+        if (a.row_weight) part.row_weight += r;
+        if (a.loss) part.loss += r;
+        if (a.dz) part.dz = static_cast<char *>(a.dz) + r * a.lddz * size;
+        const hipError_t e = launch_rows(part, st);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace zo

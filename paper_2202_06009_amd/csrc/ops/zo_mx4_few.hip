@@ -175,6 +175,17 @@ static int split_of(int64_t tiles, int64_t kt)
     return ks;
 }
 
+static int64_t few_groups(int64_t tiles, int ks)
+{
+    return (tiles + kWaves / ks - 1) / (kWaves / ks);
+}
+
+bool mx4_few_fits(int64_t n, int64_t k)
+{
+    const int64_t tiles = (n + 15) / 16;
+    return fits_a_launch(few_groups(tiles, split_of(tiles, (k + 127) / 128)), kWaves * 64);
+}
+
 template <int GX, int GT, int MB, bool FUSED>
 static hipError_t launch_split(const Mx4View &a, const void *x, int64_t ldx, const Mx4View &b,
                                void *out, int64_t ld, hipStream_t st)
@@ -182,7 +193,7 @@ static hipError_t launch_split(const Mx4View &a, const void *x, int64_t ldx, con
     const int64_t tiles = (b.rows + 15) / 16;
     const int ks = split_of(tiles, b.kt);
     const uint32_t lds = (FUSED ? (uint32_t)b.kt * 64 * 17 : 0) + (ks > 1 ? MB * kWaves * 1024 : 0);
-    const dim3 grid((uint32_t)((tiles + kWaves / ks - 1) / (kWaves / ks)));
+    const dim3 grid((uint32_t)few_groups(tiles, ks));
     const auto *px = static_cast<const typename Elem<GX>::T *>(x);
     auto *po = static_cast<typename Elem<GT>::T *>(out);
     if (ks == 1)

@@ -364,7 +364,6 @@ static hipError_t launch_tiles(const Mx4View &a, const Mx4View &b, void *out, in
     constexpr uint32_t lds = 3 * (2 * MT + WN * NT) * 1024;
     const int64_t nt = (b.rows + 16 * WN * NT - 1) / (16 * WN * NT);
     const int64_t mt = (a.rows + 32 * MT - 1) / (32 * MT), tiles = mt * nt;
-    if (tiles > INT32_MAX || a.kt > INT32_MAX) return hipErrorInvalidValue;
     const auto kernel = a.kt % 2 ? k_mx4_product<GT, MT, NT, WN, true, STREAM>
                                  : k_mx4_product<GT, MT, NT, WN, false, STREAM>;
     const hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), lds);
@@ -374,15 +373,20 @@ static hipError_t launch_tiles(const Mx4View &a, const Mx4View &b, void *out, in
     return hipGetLastError();
 }
 
+// How many of the large tiles are not halved.
+static int64_t whole_tiles(int64_t tiles)
+{
+    const int64_t rest = tiles % kCus;
+    return rest <= kCus / 2 && tiles > kCus ? tiles - rest : tiles;
+}
+
 template <int GT>
 static hipError_t launch_large(const Mx4View &a, const Mx4View &b, void *out, int64_t ld,
                                hipStream_t st)
 {
     constexpr uint32_t lds = 3 * 32 * 1024;
     const int64_t mt = (a.rows + 255) / 256, nt = (b.rows + 255) / 256, tiles = mt * nt;
-    if (tiles > INT32_MAX || a.kt > INT32_MAX) return hipErrorInvalidValue;
-    const int64_t rest = tiles % kCus;
-    const int64_t whole = rest <= kCus / 2 && tiles > kCus ? tiles - rest : tiles;
+    const int64_t whole = whole_tiles(tiles);
     const auto kernel = a.kt % 2 ? k_mx4_product_large<GT, true> : k_mx4_product_large<GT, false>;
     const hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), lds);
     if (e != hipSuccess) return e;
@@ -392,36 +396,64 @@ static hipError_t launch_large(const Mx4View &a, const Mx4View &b, void *out, in
     return hipGetLastError();
 }
 
+enum class Form { kFew, kLarge, kMiddle, kSmall };
+
+static int64_t tiles_of(int64_t m, int64_t n, int64_t tile_m, int64_t tile_n)
+{
+    return (m + tile_m - 1) / tile_m * ((n + tile_n - 1) / tile_n);
+}
+
+// Large tiles need less of memory and LDS per product: they pay from two thirds of
+// a round of the GPU on, if the steps are many for the time that a workgroup, alone
+// on its CU, takes to write its results; then 128 x 128 while that occupies half of the
+// GPU, then 128 x 64.  Measured both sides, us, large / 128 x 128:
+//   16 bits: 8192 x 6400 by 1600 67.7 / 70.2, by 800 47.5 / 44.1, by 128 28.1 / 24.1;
+//   4096 x 4096 by 1024 17.4 / 17.9; 8192 x 1600 by 6400 55 / 69
+//   32 bits: 8192 x 6400 by 2560 106 / 104, by 1600 81 / 76, by 800 61 / 50; 4096 x 4096
+//   by 2048 29.3 / 30.5; 8192 x 1600 by 6400 56 / 70
+//   32 bits, rows off the lines: 8192 x 6402 by 800 74 / 87; 4096 x 50257 by 256 243 / 215
+// 2047 x 4096 by 1024, 128 large tiles: 15.3 / 12.6 on an earlier form.  128 x 128 /
+// 128 x 64, on the same: 300 x 6400 by 1600, 150 tiles of 128 x 128, 8.5 / 9.8;
+// 2047 x 1024 by 4096, 128 of them, 15.3 / 13.3.
+static Form form_of(int64_t m, int64_t n, int64_t kt, bool f32, bool stream)
+{
+    if (m <= kFewRows) return Form::kFew;
+    if (tiles_of(m, n, 256, 256) >= 168 && kt >= (!f32 ? 8 : stream ? 20 : 3)) return Form::kLarge;
+    return tiles_of(m, n, 128, 128) >= 144 ? Form::kMiddle : Form::kSmall;
+}
+
+bool mx4_product_fits(int64_t m, int64_t n, int64_t k, int gt, const void *out, int64_t ld)
+{
+    if (m == 0 || n == 0) return true;
+    const bool stream = gt == GT_F32 ? streamed<GT_F32>(out, ld) : streamed<GT_BF16>(out, ld);
+    switch (form_of(m, n, (k + 127) / 128, gt == GT_F32, stream)) {
+    case Form::kFew: return mx4_few_fits(n, k);
+    case Form::kLarge: {
+        const int64_t tiles = tiles_of(m, n, 256, 256);
+        return fits_a_launch(2 * tiles - whole_tiles(tiles), 512);
+    }
+    case Form::kMiddle: return fits_a_launch(tiles_of(m, n, 128, 128), 256);
+    default: return fits_a_launch(tiles_of(m, n, 128, 64), 128);
+    }
+}
+
 hipError_t launch_mx4_product(const Mx4View &a, const Mx4View &b, void *out, int gt, int64_t ld,
                               hipStream_t st)
 {
     if (a.rows == 0 || b.rows == 0) return hipSuccess;
     if (a.rows <= kFewRows) return launch_mx4_few(a, b, out, gt, ld, st);
-    // Large tiles need less of memory and LDS per product: they pay from two thirds of
-    // a round of the GPU on, if the steps are many for the time that a workgroup, alone
-    // on its CU, takes to write its results; then 128 x 128 while that occupies half of the
-    // GPU, then 128 x 64.  Measured both sides, us, large / 128 x 128:
-    //   16 bits: 8192 x 6400 by 1600 67.7 / 70.2, by 800 47.5 / 44.1, by 128 28.1 / 24.1;
-    //   4096 x 4096 by 1024 17.4 / 17.9; 8192 x 1600 by 6400 55 / 69
-    //   32 bits: 8192 x 6400 by 2560 106 / 104, by 1600 81 / 76, by 800 61 / 50; 4096 x 4096
-    //   by 2048 29.3 / 30.5; 8192 x 1600 by 6400 56 / 70
-    //   32 bits, rows off the lines: 8192 x 6402 by 800 74 / 87; 4096 x 50257 by 256 243 / 215
-    // 2047 x 4096 by 1024, 128 large tiles: 15.3 / 12.6 on an earlier form.  128 x 128 /
-    // 128 x 64, on the same: 300 x 6400 by 1600, 150 tiles of 128 x 128, 8.5 / 9.8;
-    // 2047 x 1024 by 4096, 128 of them, 15.3 / 13.3.
-    const auto count = [&](int64_t m, int64_t n) {
-        return (a.rows + m - 1) / m * ((b.rows + n - 1) / n);
-    };
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
         const bool stream = streamed<GT>(out, ld);
-        if (count(256, 256) >= 168 && a.kt >= (GT != GT_F32 ? 8 : stream ? 20 : 3))
-            return launch_large<GT>(a, b, out, ld, st);
-        if (count(128, 128) >= 144)
+        switch (form_of(a.rows, b.rows, a.kt, GT == GT_F32, stream)) {
+        case Form::kLarge: return launch_large<GT>(a, b, out, ld, st);
+        case Form::kMiddle:
             return stream ? launch_tiles<GT, 4, 4, 2, true>(a, b, out, ld, st)
                           : launch_tiles<GT, 4, 4, 2, false>(a, b, out, ld, st);
-        return stream ? launch_tiles<GT, 4, 4, 1, true>(a, b, out, ld, st)
-                      : launch_tiles<GT, 4, 4, 1, false>(a, b, out, ld, st);
+        default:
+            return stream ? launch_tiles<GT, 4, 4, 1, true>(a, b, out, ld, st)
+                          : launch_tiles<GT, 4, 4, 1, false>(a, b, out, ld, st);
+        }
     });
 }
 

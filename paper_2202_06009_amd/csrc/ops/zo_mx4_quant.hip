@@ -188,6 +188,24 @@ __global__ __launch_bounds__(256) void k_mx4_quantize(const typename Elem<GT>::T
     }
 }
 
+// Row tiles of the launch; the column form covers whole tiles of 128 rows (its padding
+// columns).
+static int64_t quantize_row_tiles(int64_t rows, bool transposed, int tile)
+{
+    return ((transposed ? (rows + 127) / 128 * 128 : rows) + tile - 1) / tile;
+}
+
+bool mx4_quantize_fits(int gt, int64_t rows, int64_t cols, bool transposed)
+{
+    const int tile = gt == GT_F32 ? kTileRows<GT_F32> : kTileRows<GT_BF16>;
+    return fits_a_launch(quantize_row_tiles(rows, transposed, tile) * ((cols + 127) / 128), 256);
+}
+
+bool mx4_dequantize_fits(int64_t rows, int64_t cols)
+{
+    return fits_a_launch((rows + 63) / 64 * ((cols + 127) / 128), 256);
+}
+
 hipError_t launch_mx4_quantize(const void *x, int gt, int64_t rows, int64_t cols, int64_t ld,
                                const Mx4View *q, const Mx4View *qt, hipStream_t st)
 {
@@ -195,10 +213,7 @@ hipError_t launch_mx4_quantize(const void *x, int gt, int64_t rows, int64_t cols
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
         const int64_t ct = (cols + 127) / 128;
-        // the column form covers whole tiles of 128 rows (its padding columns)
-        const int64_t covered = qt ? (rows + 127) / 128 * 128 : rows;
-        const int64_t tiles = (covered + kTileRows<GT> - 1) / kTileRows<GT> * ct;
-        if (tiles > INT32_MAX) return hipErrorInvalidValue;
+        const int64_t tiles = quantize_row_tiles(rows, qt != nullptr, kTileRows<GT>) * ct;
         const auto *p = static_cast<const typename Elem<GT>::T *>(x);
         const Mx4View none{};
         if (q && qt)
@@ -295,7 +310,6 @@ hipError_t launch_mx4_dequantize(const Mx4View &q, void *out, int gt, int64_t ld
 {
     if (q.rows == 0 || q.cols == 0) return hipSuccess;
     const int64_t tiles = (q.rows + 63) / 64 * q.kt;
-    if (tiles > INT32_MAX) return hipErrorInvalidValue;
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
         auto *p = static_cast<typename Elem<GT>::T *>(out);

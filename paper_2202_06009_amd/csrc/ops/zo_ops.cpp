@@ -59,12 +59,6 @@ zo::Mx4View view(const zo_mx4 *q)
     return {(uint8_t *)q->codes, (uint8_t *)q->scales, q->rows, q->cols, (q->cols + 127) / 128};
 }
 
-// A workgroup takes at least 64 rows of 128 columns of a matrix.
-bool fits_a_launch(int64_t rows, int64_t cols)
-{
-    return ((rows + 127) / 128 * 2) * ((cols + 127) / 128) <= INT32_MAX;
-}
-
 }  // namespace
 
 extern "C" {
@@ -94,7 +88,7 @@ int zo_mx4_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, in
     if (qt && (qt->rows != cols || qt->cols != rows)) return ZO_EINVAL;
     if (q && (rc = check_mx4(q))) return rc;
     if (qt && (rc = check_mx4(qt))) return rc;
-    if (!fits_a_launch(rows, cols)) return ZO_EINVAL;
+    if (!zo::mx4_quantize_fits(gt, rows, cols, qt != nullptr)) return ZO_EINVAL;
     zo::Mx4View v{}, vt{};
     if (q) v = view(q);
     if (qt) vt = view(qt);
@@ -108,7 +102,7 @@ int zo_mx4_dequantize(const zo_mx4 *q, void *out, int32_t dtype, int64_t ld, hip
     if (rc) return rc;
     const int gt = elem(dtype);
     if ((rc = check_matrix(out, gt, q->rows, q->cols, ld))) return rc;
-    if (!fits_a_launch(q->rows, q->cols)) return ZO_EINVAL;
+    if (!zo::mx4_dequantize_fits(q->rows, q->cols)) return ZO_EINVAL;
     return from_hip(zo::launch_mx4_dequantize(view(q), out, gt, ld, stream));
 }
 
@@ -121,7 +115,7 @@ int zo_mx4_product(const zo_mx4 *a, const zo_mx4 *b, void *out, int32_t dtype, i
     if (a->cols != b->cols) return ZO_EINVAL;
     const int gt = elem(dtype);
     if ((rc = check_matrix(out, gt, a->rows, b->rows, ld))) return rc;
-    if (!fits_a_launch(a->rows, b->rows)) return ZO_EINVAL;
+    if (!zo::mx4_product_fits(a->rows, b->rows, a->cols, gt, out, ld)) return ZO_EINVAL;
     return from_hip(zo::launch_mx4_product(view(a), view(b), out, gt, ld, stream));
 }
 
@@ -135,10 +129,12 @@ int zo_mx4_linear(const void *x, int32_t dtype, int64_t ldx, const zo_mx4 *w, co
     const int gx = elem(dtype), go = elem(out_dtype);
     if ((rc = check_matrix(x, gx, xq->rows, xq->cols, ldx))) return rc;
     if ((rc = check_matrix(out, go, xq->rows, w->rows, ldo))) return rc;
-    if (!fits_a_launch(xq->rows, w->rows) || !fits_a_launch(xq->rows, xq->cols))
+    const bool fused = zo::few_fused(xq->rows, xq->cols);
+    if (!zo::mx4_product_fits(xq->rows, w->rows, w->cols, go, out, ldo) ||
+        (!fused && !zo::mx4_quantize_fits(gx, xq->rows, xq->cols, false)))
         return ZO_EINVAL;
     const zo::Mx4View v = view(xq);
-    if (v.rows && w->rows && zo::few_fused(v.rows, v.cols))
+    if (v.rows && w->rows && fused)
         return from_hip(zo::launch_mx4_few_fused(x, gx, v.rows, v.cols, ldx, view(w), out, go, ldo,
                                                  stream));
     rc = from_hip(zo::launch_mx4_quantize(x, gx, xq->rows, xq->cols, ldx, &v, nullptr, stream));

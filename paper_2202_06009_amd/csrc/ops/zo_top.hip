@@ -450,9 +450,8 @@ static hipError_t launch_k_top(const TopArgs &a, hipStream_t st)
     return hipGetLastError();
 }
 
-hipError_t launch_top_logits(const TopArgs &a, int gt, hipStream_t st)
+static hipError_t launch_rows(const TopArgs &a, int gt, hipStream_t st)
 {
-    if (a.rows == 0) return hipSuccess;
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
         const int64_t vecs = a.vocab / Elem<GT>::kVec;
@@ -471,6 +470,26 @@ hipError_t launch_top_logits(const TopArgs &a, int gt, hipStream_t st)
         if (a.top <= 768 && vecs <= 768 * 11) return launch_k_top<GT, 768, 11>(a, st);
         return launch_k_top<GT, 1024, 16>(a, st);
     });
+}
+
+hipError_t launch_top_logits(const TopArgs &a, int gt, hipStream_t st)
+{
+    const int64_t size = gt == GT_F32 ? 4 : 2;
+    for (int64_t r = 0; r < a.rows; r += kLaunchRows) {
+        const int64_t rows = a.rows - r < kLaunchRows ? a.rows - r : kLaunchRows;
+        const TopArgs part = {static_cast<const char *>(a.z) + r * a.ld * size,
+                              rows,
+                              a.vocab,
+                              a.ld,
+                              a.top,
+                              a.tau,
+                              a.values + r * a.top,
+                              a.columns + r * a.top,
+                              a.lse ? a.lse + r : nullptr};
+        const hipError_t e = launch_rows(part, gt, st);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace zo
