@@ -558,23 +558,21 @@ __global__ __launch_bounds__(TH, 4) void k_distill(zo_distill a)
 }
 
 template <int GT, LabelForm F>
-static void launch_form(const zo_distill &a, hipStream_t st)
+static hipError_t launch_form(const zo_distill &a, hipStream_t st)
 {
     const int64_t vecs = a.vocab / Elem<GT>::kVec;
     const uint32_t lds = (uint32_t)((a.vocab + 31) / 32 * 4);
-    const dim3 grid((uint32_t)a.rows);
     if (vecs > 1024 * 16)
-        k_distill_long<GT, F><<<grid, 1024, lds, st>>>(a);
-    else if (vecs > 512 * 16)
-        k_distill<GT, F, 1024, 16><<<grid, 1024, lds, st>>>(a);
-    else if (vecs > 512 * 8)
-        k_distill<GT, F, 512, 16><<<grid, 512, lds, st>>>(a);
-    else if (vecs > 256 * 8)
-        k_distill<GT, F, 512, 8><<<grid, 512, lds, st>>>(a);
-    else if (vecs > 256 * 4)
-        k_distill<GT, F, 256, 8><<<grid, 256, lds, st>>>(a);
-    else
-        k_distill<GT, F, 256, 4><<<grid, 256, lds, st>>>(a);
+        return start(k_distill_long<GT, F>, a.rows, 1024, lds, st, a);
+    if (vecs > 512 * 16)
+        return start(k_distill<GT, F, 1024, 16>, a.rows, 1024, lds, st, a);
+    if (vecs > 512 * 8)
+        return start(k_distill<GT, F, 512, 16>, a.rows, 512, lds, st, a);
+    if (vecs > 256 * 8)
+        return start(k_distill<GT, F, 512, 8>, a.rows, 512, lds, st, a);
+    if (vecs > 256 * 4)
+        return start(k_distill<GT, F, 256, 8>, a.rows, 256, lds, st, a);
+    return start(k_distill<GT, F, 256, 4>, a.rows, 256, lds, st, a);
 }
 
 static hipError_t launch_rows(const zo_distill &a, hipStream_t st)
@@ -584,12 +582,9 @@ static hipError_t launch_rows(const zo_distill &a, hipStream_t st)
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
         if (!labels || a.tau == 1.0f)
-            launch_form<GT, kSame>(a, st);
-        else if (a.tau == 2.0f)
-            launch_form<GT, kSquare>(a, st);
-        else
-            launch_form<GT, kOwn>(a, st);
-        return hipGetLastError();
+            return launch_form<GT, kSame>(a, st);
+        if (a.tau == 2.0f) return launch_form<GT, kSquare>(a, st);
+        return launch_form<GT, kOwn>(a, st);
     });
 }
 

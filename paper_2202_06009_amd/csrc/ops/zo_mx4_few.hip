@@ -193,18 +193,13 @@ static hipError_t launch_split(const Mx4View &a, const void *x, int64_t ldx, con
     const int64_t tiles = (b.rows + 15) / 16;
     const int ks = split_of(tiles, b.kt);
     const uint32_t lds = (FUSED ? (uint32_t)b.kt * 64 * 17 : 0) + (ks > 1 ? MB * kWaves * 1024 : 0);
-    const dim3 grid((uint32_t)few_groups(tiles, ks));
     const auto *px = static_cast<const typename Elem<GX>::T *>(x);
     auto *po = static_cast<typename Elem<GT>::T *>(out);
-    if (ks == 1)
-        k_mx4_few<GX, GT, MB, 1, FUSED><<<grid, kWaves * 64, lds, st>>>(a, px, ldx, b, po, ld);
-    else if (ks == 2)
-        k_mx4_few<GX, GT, MB, 2, FUSED><<<grid, kWaves * 64, lds, st>>>(a, px, ldx, b, po, ld);
-    else if (ks == 4)
-        k_mx4_few<GX, GT, MB, 4, FUSED><<<grid, kWaves * 64, lds, st>>>(a, px, ldx, b, po, ld);
-    else
-        k_mx4_few<GX, GT, MB, 8, FUSED><<<grid, kWaves * 64, lds, st>>>(a, px, ldx, b, po, ld);
-    return hipGetLastError();
+    const auto kernel = ks == 1   ? k_mx4_few<GX, GT, MB, 1, FUSED>
+                        : ks == 2 ? k_mx4_few<GX, GT, MB, 2, FUSED>
+                        : ks == 4 ? k_mx4_few<GX, GT, MB, 4, FUSED>
+                                  : k_mx4_few<GX, GT, MB, 8, FUSED>;
+    return start(kernel, few_groups(tiles, ks), kWaves * 64, lds, st, a, px, ldx, b, po, ld);
 }
 
 hipError_t launch_mx4_few(const Mx4View &a, const Mx4View &b, void *out, int gt, int64_t ld,

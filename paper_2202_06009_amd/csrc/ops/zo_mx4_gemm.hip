@@ -368,9 +368,8 @@ static hipError_t launch_tiles(const Mx4View &a, const Mx4View &b, void *out, in
                                  : k_mx4_product<GT, MT, NT, WN, false, STREAM>;
     const hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), lds);
     if (e != hipSuccess) return e;
-    kernel<<<dim3((uint32_t)tiles), 128 * WN, lds, st>>>(
-        a, b, static_cast<typename Elem<GT>::T *>(out), ld, (uint32_t)mt, (uint32_t)nt);
-    return hipGetLastError();
+    return start(kernel, tiles, 128 * WN, lds, st, a, b, static_cast<typename Elem<GT>::T *>(out),
+                 ld, (uint32_t)mt, (uint32_t)nt);
 }
 
 // How many of the large tiles are not halved.
@@ -390,10 +389,9 @@ static hipError_t launch_large(const Mx4View &a, const Mx4View &b, void *out, in
     const auto kernel = a.kt % 2 ? k_mx4_product_large<GT, true> : k_mx4_product_large<GT, false>;
     const hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), lds);
     if (e != hipSuccess) return e;
-    kernel<<<dim3((uint32_t)(whole + 2 * (tiles - whole))), 512, lds, st>>>(
-        a, b, static_cast<typename Elem<GT>::T *>(out), ld, (uint32_t)mt, (uint32_t)nt,
-        (uint32_t)whole);
-    return hipGetLastError();
+    return start(kernel, 2 * tiles - whole, 512, lds, st, a, b,
+                 static_cast<typename Elem<GT>::T *>(out), ld, (uint32_t)mt, (uint32_t)nt,
+                 (uint32_t)whole);
 }
 
 enum class Form { kFew, kLarge, kMiddle, kSmall };

@@ -216,16 +216,11 @@ hipError_t launch_mx4_quantize(const void *x, int gt, int64_t rows, int64_t cols
         const int64_t tiles = quantize_row_tiles(rows, qt != nullptr, kTileRows<GT>) * ct;
         const auto *p = static_cast<const typename Elem<GT>::T *>(x);
         const Mx4View none{};
-        if (q && qt)
-            k_mx4_quantize<GT, true, true><<<dim3((uint32_t)tiles), 256, 0, st>>>(
-                p, rows, cols, ld, (uint32_t)ct, *q, *qt);
-        else if (q)
-            k_mx4_quantize<GT, true, false><<<dim3((uint32_t)tiles), 256, 0, st>>>(
-                p, rows, cols, ld, (uint32_t)ct, *q, none);
-        else
-            k_mx4_quantize<GT, false, true><<<dim3((uint32_t)tiles), 256, 0, st>>>(
-                p, rows, cols, ld, (uint32_t)ct, none, *qt);
-        return hipGetLastError();
+        const auto kernel = q && qt ? k_mx4_quantize<GT, true, true>
+                            : q     ? k_mx4_quantize<GT, true, false>
+                                    : k_mx4_quantize<GT, false, true>;
+        return start(kernel, tiles, 256, 0, st, p, rows, cols, ld, (uint32_t)ct, q ? *q : none,
+                     qt ? *qt : none);
     });
 }
 
@@ -313,13 +308,9 @@ hipError_t launch_mx4_dequantize(const Mx4View &q, void *out, int gt, int64_t ld
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
         auto *p = static_cast<typename Elem<GT>::T *>(out);
-        if ((uintptr_t)p % 128 == 0 && ld * sizeof(*p) % 128 == 0)
-            k_mx4_dequantize<GT, true><<<dim3((uint32_t)tiles), 256, 0, st>>>(q, p, ld,
-                                                                             (uint32_t)q.kt);
-        else
-            k_mx4_dequantize<GT, false><<<dim3((uint32_t)tiles), 256, 0, st>>>(q, p, ld,
-                                                                              (uint32_t)q.kt);
-        return hipGetLastError();
+        const bool lines = (uintptr_t)p % 128 == 0 && ld * sizeof(*p) % 128 == 0;
+        return start(lines ? k_mx4_dequantize<GT, true> : k_mx4_dequantize<GT, false>, tiles, 256,
+                     0, st, q, p, ld, (uint32_t)q.kt);
     });
 }
 

@@ -41,6 +41,22 @@ static hipError_t with_elem_type(int gt, F &&f)
     }
 }
 
+template <class T>
+struct AsIs {
+    using type = T;
+};
+
+// Launches a kernel; the launch's own error, which an error that an earlier call of the
+// program left in the runtime is not.
+template <class... P>
+static hipError_t start(void (*kernel)(P...), int64_t groups, int threads, uint32_t lds,
+                        hipStream_t st, typename AsIs<P>::type... args)
+{
+    void *at[] = {&args...};
+    return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((uint32_t)groups),
+                           dim3((uint32_t)threads), at, lds, st);
+}
+
 template <int GT>
 __device__ __forceinline__ float widen(typename Elem<GT>::T bits)
 {

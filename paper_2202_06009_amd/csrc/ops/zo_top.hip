@@ -446,8 +446,7 @@ __global__ __launch_bounds__(TH, TH == 768 ? 6 : 4) void k_top(TopArgs a)
 template <int GT, int TH, int NV>
 static hipError_t launch_k_top(const TopArgs &a, hipStream_t st)
 {
-    k_top<GT, TH, NV><<<dim3((uint32_t)a.rows), TH, 0, st>>>(a);
-    return hipGetLastError();
+    return start(k_top<GT, TH, NV>, a.rows, TH, 0, st, a);
 }
 
 static hipError_t launch_rows(const TopArgs &a, int gt, hipStream_t st)
@@ -455,10 +454,7 @@ static hipError_t launch_rows(const TopArgs &a, int gt, hipStream_t st)
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
         const int64_t vecs = a.vocab / Elem<GT>::kVec;
-        if (vecs > 1024 * 16) {
-            k_top_long<GT><<<dim3((uint32_t)a.rows), 1024, 0, st>>>(a);
-            return hipGetLastError();
-        }
+        if (vecs > 1024 * 16) return start(k_top_long<GT>, a.rows, 1024, 0, st, a);
         // the more are wanted, the more threads: about 4 groups a logit or more.  Long
         // rows: two workgroups of 768 threads a CU, 24 waves (4096 x 50257 bfloat16, 64
         // wanted: 138 us; of 512 with 16 waves 159, of 256 with 12 waves 175, of 1024
