@@ -139,7 +139,7 @@ __device__ __forceinline__ bool read_row(const zo_distill &a, Row<TH> &R, Distil
     R.row = blockIdx.x;
     R.V = a.vocab;
     R.top = a.top;
-    R.c = kLog2e / a.tau;
+    R.c = log2_factor(a.tau);
     R.tail = a.teacher_lse != nullptr;
     R.w = a.row_weight ? a.row_weight[R.row] : 1.0f;
     if (R.w == 0.0f) return false;
@@ -281,7 +281,8 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, const Row<TH> &
             kl += 1.0f - qsum;
         }
         float l = 0.0f;
-        if (t.kd) l = a.kd_weight * a.tau * a.tau * kl;
+        if (t.kd)                       // tau^2 may be 0 in binary32
+            l = kl == INFINITY ? a.kd_weight * kl : a.kd_weight * a.tau * a.tau * kl;
         if (R.y >= 0) {
             const float lz = log_above(R.zy, m_all, 1.0f, above_one<FAR, F>(R.zy, c, t));
             l += a.ce_weight * (R.zy == -INFINITY ? INFINITY : logf(t.s_one) - lz);

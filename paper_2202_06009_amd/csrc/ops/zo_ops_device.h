@@ -152,6 +152,12 @@ __device__ __forceinline__ u32x4 pack16(const float (&v)[Elem<GT>::kVec])
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
+// log2(e) / tau, finite for a tau below the normal numbers too: 0 times it is then 0.
+__device__ __forceinline__ float log2_factor(float tau)
+{
+    return fminf(kLog2e / tau, 0x1.fffffep127f);
+}
+
 // 2^x to about one unit in the last place; results below 2^-126 become 0,
 // which no sum of a softmax notices.
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }

@@ -189,7 +189,7 @@ __device__ void lse_row(const TopArgs &a, int64_t row, TopShared<TH> &s)
     constexpr int K = Elem<GT>::kVec;
     const int64_t V = a.vocab;
     const auto *z = static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ld;
-    const float c = kLog2e / a.tau;
+    const float c = log2_factor(a.tau);
     float m = -INFINITY, sum = 0.0f;
     bool nan = false;
     for (int64_t i = (int64_t)threadIdx.x * K; i < V; i += TH * K) {
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(1024) void k_top_long(TopArgs a)
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x, V = a.vocab;
     const auto *z = static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ld;
-    const float c = kLog2e / a.tau;
+    const float c = log2_factor(a.tau);
     for (int i = tid; i < 256; i += TH) s.hist[i] = 0;
     if (tid == 0) s.sel[3] = 0;
     GroupMaxima m = {-INFINITY, {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, 0};
@@ -391,7 +391,7 @@ __global__ __launch_bounds__(TH, TH == 768 ? 6 : 4) void k_top(TopArgs a)
 
     // sum of 2^(c z - r); its NaN also tells of a row with NaN or +infinity (the
     // maxima pass over NaN)
-    const float c = kLog2e / a.tau, r = reference(M, c);
+    const float c = log2_factor(a.tau), r = reference(M, c);
     float sum = term(x.last, c, r);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {

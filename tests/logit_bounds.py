@@ -155,6 +155,7 @@ def distill(z, vals, cols, dtype, *, tau=1.0, lse=None, labels=None, kd=1.0, ce=
         if abs(loss[t]) > FLT_MAX * (1 + E):
             loss[t] = np.copysign(np.inf, loss[t])
         lim_loss[t] = abs(w) * lim + (16 * E * abs(loss[t]) if np.isfinite(loss[t]) else 0.0)
+        lim_loss[t] += abs(w) * 2.0 ** -120           # below the normal numbers
         grad = abs(w) * grad + 16 * E * np.abs(dz[t])
         lim_dz[t] = grad + HALF_ULP[dtype] * (np.abs(dz[t]) + grad)
         lim_dz[t] += abs(w) * (kd * tau + ce) * 2.0 ** -120

@@ -113,3 +113,17 @@ def test_ends_of_the_type(torch, vocab, tail, tau):
         for ce in (0.0, 0.5):
             _check(torch, "float32", z, vals, cols, tau=tau, lse=lse if tail else None,
                    labels=labels, ce=ce, inplace=inplace)
+
+
+@pytest.mark.parametrize("vocab", VOCABS)
+def test_tau_below_the_normal_numbers(torch, vocab):
+    """log2(e) / tau passes binary32; q and p are those of the largest logits alone."""
+    r = np.random.default_rng(vocab)
+    z = -r.integers(0, 3, (4, vocab)).astype(np.float64)
+    z[1], z[2], z[3] = z[1] + 2.0, 0.0, z[3] - 5.0
+    cols = np.stack([r.permutation(vocab)[:5] for _ in range(4)]).astype(np.int32)
+    vals = r.integers(-1, 1, (4, 5)).astype(np.float32)
+    for tail in (False, True):
+        for ce in (0.0, 0.5):
+            _check(torch, "float32", z, vals, cols, tau=2.0 ** -133, ce=ce, labels=cols[:, 1].copy(),
+                   lse=np.log(3 * np.ones(4, np.float32)) if tail else None)

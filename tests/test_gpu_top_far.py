@@ -64,3 +64,11 @@ def test_large_logits(torch, vocab, tau):
     for z in (lb.large_rows(vocab, tau)[0], lb.extreme_rows(vocab, tau)[0]):
         for top in (1, 8, 100):
             _check(torch, "float32", z, top, tau)
+
+
+@pytest.mark.parametrize("vocab", [130, 5000, 50257, 70001])
+def test_tau_below_the_normal_numbers(torch, vocab):
+    """log2(e) / tau passes binary32: the sum is the count of the largest logits."""
+    z = -np.random.default_rng(vocab).integers(0, 3, (2, vocab)).astype(np.float64)
+    z[1] = 0.0
+    _check(torch, "float32", z, 8, 2.0 ** -133)
