@@ -216,14 +216,20 @@ hipError_t launch_mx4_few(const Mx4View &a, const Mx4View &b, void *out, int gt,
 }
 
 // Every workgroup quantises all of x, so with many tile rows a kernel of its own is
-// faster.  Measured, one kernel / two, us (rows x matrix; tile rows): 1 x 1600 x 6400 (50)
-// 5.9 / 8.6; 16 x 50257 x 1600 (208) 12.2 / 14.3; 8 x 1600 x 6400 (400) 6.4 / 8.4;
-// 8 x 6400 x 6400 (400) 12.0 / 10.2; 16 x 1600 x 6400 (800) 9.8 / 8.5; 16 x 6400 x 6400
-// (800) 17.6 / 10.6.
-bool few_fused(int64_t rows, int64_t cols)
+// faster, the sooner the more workgroups there are beside their work: where eight waves
+// share 16 rows of the matrix and there are more workgroups than CUs, from 200 tile rows
+// on, otherwise from 400.  Measured, one kernel / two, us (rows x matrix; tile rows):
+//   8 x 6400 x 2560 (160) 5.7 / 6.6; 11 x 6400 x 2560 (220) 6.7 / 6.5; 8 x 6400 x 4096 (256)
+//   8.6 / 8.4; 8 x 6400 x 6400 (400) 12.1 / 10.5
+//   8 x 4096 x 6400 (400) 8.1 / 9.6; 16 x 4096 x 4096 (512) 7.6 / 7.0; 16 x 1600 x 6400 (800)
+//   9.8 / 8.0; 16 x 25600 x 2560 (320) 12.0 / 12.3; 16 x 50257 x 1600 (208) 12.1 / 14.5;
+//   1 x 6400 x 1600 (13) 4.1 / 6.6
+bool few_fused(int64_t rows, int64_t n, int64_t k)
 {
-    const int64_t kt = (cols + 127) / 128;
-    return rows <= 16 && kt <= kFusedTiles && rows * kt <= 400;
+    const int64_t kt = (k + 127) / 128, tiles = (n + 15) / 16;
+    const int ks = split_of(tiles, kt);
+    const bool crowded = ks == kWaves && few_groups(tiles, ks) > 256;
+    return rows <= 16 && kt <= kFusedTiles && rows * kt <= (crowded ? 200 : 400);
 }
 
 hipError_t launch_mx4_few_fused(const void *x, int gx, int64_t rows, int64_t cols, int64_t ldx,

@@ -129,7 +129,7 @@ int zo_mx4_linear(const void *x, int32_t dtype, int64_t ldx, const zo_mx4 *w, co
     const int gx = elem(dtype), go = elem(out_dtype);
     if ((rc = check_matrix(x, gx, xq->rows, xq->cols, ldx))) return rc;
     if ((rc = check_matrix(out, go, xq->rows, w->rows, ldo))) return rc;
-    const bool fused = zo::few_fused(xq->rows, xq->cols);
+    const bool fused = zo::few_fused(xq->rows, w->rows, xq->cols);
     if (!zo::mx4_product_fits(xq->rows, w->rows, w->cols, go, out, ldo) ||
         (!fused && !zo::mx4_quantize_fits(gx, xq->rows, xq->cols, false)))
         return ZO_EINVAL;

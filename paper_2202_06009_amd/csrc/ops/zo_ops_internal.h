@@ -35,12 +35,13 @@ hipError_t launch_mx4_dequantize(const Mx4View &q, void *out, int gt, int64_t ld
 hipError_t launch_mx4_product(const Mx4View &a, const Mx4View &b, void *out, int gt, int64_t ld,
                               hipStream_t st);
 // The products of few rows of a (at most kFewRows) by b; from activations x of
-// element type gx that the kernel quantises itself, where few_fused says so.
+// element type gx that the kernel quantises itself, where few_fused says so of
+// [rows, k] by [n, k].
 constexpr int kFewRows = 64;
 bool mx4_few_fits(int64_t n, int64_t k);
 hipError_t launch_mx4_few(const Mx4View &a, const Mx4View &b, void *out, int gt, int64_t ld,
                           hipStream_t st);
-bool few_fused(int64_t rows, int64_t cols);
+bool few_fused(int64_t rows, int64_t n, int64_t k);
 hipError_t launch_mx4_few_fused(const void *x, int gx, int64_t rows, int64_t cols, int64_t ldx,
                                 const Mx4View &b, void *out, int gt, int64_t ld, hipStream_t st);
 

@@ -72,3 +72,21 @@ def test_product_in_binary16(torch, m, n, k, pad):
     off = (full[:, :n].double() - want).abs()
     assert bool((off <= acc + HALF_ULP["float16"] * (want.abs() + acc) + 2.0 ** -25).all())
     assert (full[:, n:] == 7).all()
+
+
+@pytest.mark.parametrize("m", [1, 7, 8, 11, 16])
+@pytest.mark.parametrize("n,k", [(6400, 2560), (6400, 6400), (4096, 6400), (4113, 4000), (25600, 512),
+                                 (517, 6656), (130, 6657)])
+def test_linear_is_quantize_and_product(torch, m, n, k):
+    """The one-kernel form and the two kernels, on both sides of where one gives way to the
+    other: the same bits."""
+    import paper_2202_06009_amd as zo
+    x = torch.randn((m, k), device="cuda").bfloat16()
+    w = zo.Mx4(n, k)
+    zo.zo_mx4_quantize(torch.randn((n, k), device="cuda"), w)
+    one, two = (torch.full((m, n), 7.0, device="cuda") for _ in range(2))
+    xq = zo.Mx4(m, k)
+    zo.zo_mx4_linear(x, w, one, zo.Mx4(m, k))
+    zo.zo_mx4_quantize(x, xq)
+    zo.zo_mx4_product(xq, w, two)
+    assert torch.equal(one, two)
