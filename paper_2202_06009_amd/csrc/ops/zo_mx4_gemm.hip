@@ -401,23 +401,36 @@ static int64_t tiles_of(int64_t m, int64_t n, int64_t tile_m, int64_t tile_n)
     return (m + tile_m - 1) / tile_m * ((n + tile_n - 1) / tile_n);
 }
 
-// Large tiles need less of memory and LDS per product: they pay from two thirds of
-// a round of the GPU on, if the steps are many for the time that a workgroup, alone
-// on its CU, takes to write its results; then 128 x 128 while that occupies half of the
-// GPU, then 128 x 64.  Measured both sides, us, large / 128 x 128:
-//   16 bits: 8192 x 6400 by 1600 67.7 / 70.2, by 800 47.5 / 44.1, by 128 28.1 / 24.1;
-//   4096 x 4096 by 1024 17.4 / 17.9; 8192 x 1600 by 6400 55 / 69
-//   32 bits: 8192 x 6400 by 2560 106 / 104, by 1600 81 / 76, by 800 61 / 50; 4096 x 4096
-//   by 2048 29.3 / 30.5; 8192 x 1600 by 6400 56 / 70
-//   32 bits, rows off the lines: 8192 x 6402 by 800 74 / 87; 4096 x 50257 by 256 243 / 215
-// 2047 x 4096 by 1024, 128 large tiles: 15.3 / 12.6 on an earlier form.  128 x 128 /
-// 128 x 64, on the same: 300 x 6400 by 1600, 150 tiles of 128 x 128, 8.5 / 9.8;
-// 2047 x 1024 by 4096, 128 of them, 15.3 / 13.3.
+// Large tiles need less of memory and LDS per product and take a CU each; of 128 x 128 a
+// CU takes three.  Large ones pay where they make one round of the GPU and the others
+// more than one, or from one and a half rounds on, if the steps are many for the time that
+// a workgroup, alone on its CU, takes to write its results (the more so in 32 bits on lines,
+// where the others' stores go past the caches); with many steps, from two thirds of a
+// round on.  Otherwise 128 x 128 while that occupies half of the GPU, then 128 x 64.
+// Measured both sides in a graph, outputs in turn, us, large / 128 x 128:
+//   175 tiles, 6400 x 1600: 16 bits by 1600 20.5 / 18.2, by 6400 1% under; 32 bits by 6400
+//   57.9 / 57.0; 196 off the lines, 812 x 12547 by 4640 49.9 / 54.0; 192, 6144 x 2048 by 1600
+//   19.9 / 18.8; 320, 5120 x 4096 by 2560 48.4 / 42.0
+//   200 (800 of the others), 10208 x 1239 by 4007 45.6 / 53.4; 208, 6656 x 2048: 16 bits by
+//   1024 17.1 / 17.9; 32 bits by 1280 23.5 / 23.9; 224, 8192 x 1600 by 6400 55.6 / 74.2
+//   16 bits on lines: 8192 x 6400 by 1024 54.1 / 51.0, by 2560 2% under; 10240 x 4096 by 1280
+//   52.1 / 46.9, by 4096 2% under; 8192 x 4096 by 1600 45.1 / 47.9
+//   32 bits on lines: 8192 x 4096 by 2560 77.9 / 70.9, by 4096 102.7 / 103.7
+//   off the lines: 4096 x 50257 in 16 bits by 1024 240 / 256, in 32 328 / 362; 8192 x 4098 in
+//   32 bits by 768 49.5 / 57.2
+// 128 x 128 / 128 x 64: 144 tiles, 1152 x 2048 by 1600 9.0 / 10.6; 128, 2047 x 1024 by 4096
+// 16.6 / 15.0, by 512 6.1 / 5.7.
 static Form form_of(int64_t m, int64_t n, int64_t kt, bool f32, bool stream)
 {
     if (m <= kFewRows) return Form::kFew;
-    if (tiles_of(m, n, 256, 256) >= 168 && kt >= (!f32 ? 8 : stream ? 20 : 3)) return Form::kLarge;
-    return tiles_of(m, n, 128, 128) >= 144 ? Form::kMiddle : Form::kSmall;
+    const int64_t large = tiles_of(m, n, 256, 256), middle = tiles_of(m, n, 128, 128);
+    const bool fills = large <= kCus ? middle > 3 * kCus : large >= kCus * 3 / 2;
+    const int64_t steps = !stream        ? (f32 ? 3 : 8)
+                          : large > kCus ? (f32 ? 32 : 16)
+                                         : (f32 ? 10 : 8);
+    if (fills && kt >= steps) return Form::kLarge;
+    if (large >= 168 && large <= kCus && kt >= 32 && !(f32 && stream)) return Form::kLarge;
+    return middle >= 144 ? Form::kMiddle : Form::kSmall;
 }
 
 bool mx4_product_fits(int64_t m, int64_t n, int64_t k, int gt, const void *out, int64_t ld)

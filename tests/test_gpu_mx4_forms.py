@@ -46,13 +46,7 @@ def test_dequantize_on_lines(torch, shape, dtype):
         assert (full[:, :off] == 7).all() and (full[:, off + cols:] == 7).all()
 
 
-# large tiles with an even and an odd number of steps, whole rounds and a rest, then
-# 128 x 128 and 128 x 64
-@pytest.mark.parametrize("m,n,k", [(4200, 4303, 1020), (2500, 7296, 1300), (2050, 8200, 1024),
-                                   (6333, 1601, 1200), (2300, 7300, 200), (1000, 2000, 300),
-                                   (300, 500, 700)])
-@pytest.mark.parametrize("pad", [0, 1, 64])
-def test_product_in_binary16(torch, m, n, k, pad):
+def _check_product(torch, m, n, k, pad, dtype):
     import paper_2202_06009_amd as zo
     g = torch.Generator(device="cuda").manual_seed(m + n)
     a = torch.randn((m, k), generator=g, device="cuda")
@@ -64,14 +58,34 @@ def test_product_in_binary16(torch, m, n, k, pad):
     zo.zo_mx4_dequantize(aq, va)
     zo.zo_mx4_dequantize(bq, vb)
     wide = n + pad if pad < 64 else -(-n // 64) * 64
-    full = torch.full((m, wide), 7.0, dtype=torch.float16, device="cuda")
+    full = torch.full((m, wide), 7.0, dtype=getattr(torch, dtype), device="cuda")
     zo.zo_mx4_product(aq, bq, full[:, :n])
     va, vb = va.double(), vb.double()
     want = va @ vb.t().contiguous()
     acc = (k + 8) * 2.0 ** -23 * (va.abs() @ vb.abs().t().contiguous())
     off = (full[:, :n].double() - want).abs()
-    assert bool((off <= acc + HALF_ULP["float16"] * (want.abs() + acc) + 2.0 ** -25).all())
+    tiny = 2.0 ** -25 if dtype == "float16" else 2.0 ** -134
+    assert bool((off <= acc + HALF_ULP[dtype] * (want.abs() + acc) + tiny).all())
     assert (full[:, n:] == 7).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(4200, 4303, 1020), (2500, 7296, 1300), (2050, 8200, 1024),
+                                   (6333, 1601, 1200), (2300, 7300, 200), (1000, 2000, 300),
+                                   (300, 500, 700)])
+@pytest.mark.parametrize("pad", [0, 1, 64])
+def test_product_in_binary16(torch, m, n, k, pad):
+    _check_product(torch, m, n, k, pad, "float16")
+
+
+# tiles of 256 x 256: 221 of one round, 384 and 544 of several with a rest that is halved, 420
+# with one that is not; steps around the least for each, odd and even
+@pytest.mark.parametrize("m,n,k", [(3300, 4350, 1100), (3300, 4350, 1500), (6100, 4050, 2090),
+                                   (6100, 4050, 4200), (8100, 4200, 2000), (8100, 4200, 1900),
+                                   (5333, 5097, 2433), (5333, 5097, 4100)])
+@pytest.mark.parametrize("pad", [0, 64])
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+def test_product_of_large_tiles(torch, m, n, k, pad, dtype):
+    _check_product(torch, m, n, k, pad, dtype)
 
 
 @pytest.mark.parametrize("m", [1, 7, 8, 11, 16])
