@@ -249,7 +249,7 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, const Row<TH> &
         if (p == 0.0f)
             kl += q;
         else if (t.none || z == -INFINITY)
-            kl = INFINITY;
+            kl += INFINITY;
         else
             kl += p * (logp - (log_above(z, m_all, a.tau, l) - log_all)) - p + q;
         qsum += q;
@@ -268,7 +268,7 @@ __device__ __forceinline__ Stats statistics(const zo_distill &a, const Row<TH> &
             // log(pr / qr) from the logarithms where qr is near the end of binary32 or past it
             const float qr = t.s_out * t.share;
             if (t.pr > 0.0f && t.no_rest)
-                kl = INFINITY;
+                kl += INFINITY;
             else if (t.pr > 0.0f && qr < 0x1p-100f)
                 kl += t.pr * (logf(t.pr) - (log_between<FAR>(t.b_out, t.b_all, c, a.tau) +
                                             logf(t.s_out / t.s_all))) - t.pr + qr;

@@ -127,3 +127,22 @@ def test_tau_below_the_normal_numbers(torch, vocab):
         for ce in (0.0, 0.5):
             _check(torch, "float32", z, vals, cols, tau=2.0 ** -133, ce=ce, labels=cols[:, 1].copy(),
                    lse=np.log(3 * np.ones(4, np.float32)) if tail else None)
+
+
+@pytest.mark.parametrize("vocab", VOCABS)
+def test_not_a_number_is_not_hidden(torch, vocab):
+    """A NaN in a used slot, with everything else excluded and mass of the teacher there;
+    one outside S; the rows beside them keep theirs."""
+    import paper_2202_06009_amd as zo
+    z = torch.full((4, vocab), -float("inf"), device="cuda")
+    cols = torch.tensor([[3, 7]] * 4, dtype=torch.int32, device="cuda")
+    z[:, 3], z[:, 7] = 1.0, 2.0
+    z[0, 3] = float("nan")
+    z[1, 11] = float("nan")
+    z[3, 20] = 0.5
+    loss, dz = torch.zeros(4, device="cuda"), torch.zeros_like(z)
+    zo.zo_distill_loss(z, torch.ones((4, 2), device="cuda"), cols, loss, dz,
+                       teacher_lse=torch.full((4,), 2.0, device="cuda"))
+    assert torch.isnan(loss).tolist() == [True, True, False, False]
+    assert loss[2] == float("inf") and torch.isfinite(loss[3])
+    assert torch.isfinite(dz[2:]).all()
