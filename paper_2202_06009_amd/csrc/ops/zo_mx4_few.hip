@@ -1,6 +1,7 @@
 // zo_mx4_few.hip -- products of a few rows (a decode step) by a 4-bit matrix.
 //
-// The bound is reading the matrix once: 17/32 bytes an element.  A wave takes 16
+// The bound is reading the matrix once: 17/32 bytes an element (1 x 50257 x 1600 9.4 us,
+// 4.6 TB/s; 11 rows 11.4 us, their quantisation before the stream).  A wave takes 16
 // of its rows, 1 KiB a tile of 128 columns in one access per lane, and keeps
 // eight tiles in flight; where the matrix has too few rows to occupy the GPU, the
 // KS waves of a group share them, each a run of the tiles, and their sums are

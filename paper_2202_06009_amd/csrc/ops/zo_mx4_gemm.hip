@@ -1,7 +1,8 @@
 // zo_mx4_gemm.hip -- products of microscaled 4-bit matrices on the scaled matrix
-// instruction (32 x 32 x 64, E2M1 operands, binary32 accumulators).  Of the two forms
-// with 4-bit operands this one gives 8.8 PFLOP/s by itself, the 16 x 16 x 128 one 5.0 to
-// 6.5 (each instruction costs an issue slot more for its scales).
+// instruction (32 x 32 x 64, E2M1 operands, binary32 accumulators).  By itself, two waves a
+// SIMD on random operands that stay in registers, it gives 6.3 PFLOP/s over 1 to 14 ms and
+// the 16 x 16 x 128 form 6.8 (both 9.6 on operands that are all alike: the clock follows
+// the bits that change); in this kernel this form was a few percent faster.
 //
 // Operand layout of the instruction: lane l holds row l % 32, elements
 // 32 (l / 32) .. + 31 of the 64 (16 bytes), and their scale byte, one of the four bytes
@@ -141,11 +142,12 @@ __device__ __forceinline__ const uint8_t *scales_at(const Mx4View &x, int64_t gr
 // of loads are in flight, about what the memory's latency takes.
 // ODD: an odd number of steps (the register sets go round by twos).
 //
-// Measured: 16384 x 16384 by 8192 1.13 ms (3.8 PFLOP/s), 8192 x 6400 by 1600 68 us, 8192 x 1600
-// by 6400 55 us.  Bound: copies of the kernel that leave work out (on the 16 x 16 x 128
-// form) took 0.79 ms of 1.12 without any operand traffic, 0.85 without the loads and
-// the writes to shared memory, 1.02 without the reads from it: the loads (32 KiB a
-// step through the L1, about 30 bytes a clock) take the most, the matrix pipe next.
+// Measured: 16384 x 16384 by 8192 1.14 ms (3.9 PFLOP/s), 8192 x 6400 by 1600 67 us, 8192 x
+// 1600 by 6400 56 us.  Bound: copies of the kernel that leave work out took, in this order,
+// 0.79 ms (5.6 PFLOP/s), 45 and 40 us without any operand traffic, 0.84 ms, 44 and 42 us
+// without the loads and the writes to shared memory, 1.10 ms, 62 and 54 us without the
+// reads from it: the loads (32 KiB a step through the L1, about 30 bytes a clock) take the
+// most beside the matrix pipe.
 // Four waves of 128 x 128 read less of shared memory but leave no registers for loads
 // in flight (1.5 ms); workgroups of 128 x 256, two a CU, spill (1.8 ms).
 //

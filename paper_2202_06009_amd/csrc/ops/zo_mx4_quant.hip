@@ -12,7 +12,9 @@
 // workgroup takes 64 (binary32) or 128 rows of 128 columns: 16 lanes read a
 // row's 128 elements, 8 each, so that four lanes hold a block, and the four
 // 16-row passes of a 64-row group make up the dwords in which the scales are
-// stored.  For the column form the tile goes through shared memory once.
+// stored.  For the column form the tile goes through shared memory once.  8192 x 6400
+// bfloat16 both ways 34 us (4.7 TB/s), 6400 x 1600 binary32 14.1 us (3.7), 8192 x 1600
+// bfloat16 by rows 11.0 us (3.0), 8191 x 4097 binary16 both ways, off the lines, 26.0 us (4.0).
 #include "zo_mx4_device.h"
 
 namespace zo {
@@ -238,10 +240,11 @@ __device__ __forceinline__ void put16(typename Elem<GT>::T *p, const u32x4 &w, i
 // four rows a thread.  The conversion to binary32 is exact; its upper half is the bfloat16.
 //
 // NT: nontemporal stores, for rows on lines of 128 bytes, which are then written once:
-// 16384 x 8192 bfloat16 66 -> 49 us, 8191 x 4096 binary32 27.5 -> 24.6 us (7.0 TB/s).  Off
-// the lines a store touches parts of some: 8191 x 4104 binary16 16 us, 30 us nontemporal;
-// 8191 x 4097 17.6 us.  Eight elements of a lane side by side, in binary32 two stores of
-// every other 16 bytes, took 72 us for 8191 x 4096.
+// 16384 x 8192 bfloat16 61 -> 51 us (6.6 TB/s), 8191 x 4096 binary32 29.9 -> 26.1 us (5.8 TB/s).
+// Off the lines a store touches parts of some: 8191 x 4104 binary16 26.3 us, 31.6 us
+// nontemporal; 8191 x 4097 30.9 us (2.7 TB/s; outputs in turn, past the caches' size).
+// Eight elements of a lane side by side, in binary32 two stores of every other 16 bytes,
+// took 72 us for 8191 x 4096 where this took 24.6.
 template <int GT, bool NT>
 __global__ __launch_bounds__(256) void k_mx4_dequantize(Mx4View q,
                                                         typename Elem<GT>::T *__restrict__ out,
