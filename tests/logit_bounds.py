@@ -101,6 +101,7 @@ def distill(z, vals, cols, dtype, *, tau=1.0, lse=None, labels=None, kd=1.0, ce=
             else:
                 logp = u / tau - float(lse[t])
                 p = np.exp(logp)
+            p = np.where(p < 2.0 ** -150, 0.0, p)     # as binary32 has it
             kl = _loss_of(p, logp, logq[at])
             d = q.copy()
             d[at] -= p
