@@ -33,6 +33,9 @@ EXPORTS = (
     "zo_config_check", "zo_plan_num_chunks", "zo_plan_chunks",
     "zo_mx4_code_bytes", "zo_mx4_scale_bytes", "zo_mx4_quantize", "zo_mx4_dequantize",
     "zo_mx4_product", "zo_mx4_linear", "zo_top_logits", "zo_distill_loss",
+    "zo_i8_code_bytes", "zo_i8_work_bytes", "zo_i8_quantize", "zo_i8_dequantize",
+    "zo_i8_product", "zo_i8_linear", "zo_rms_norm", "zo_rms_norm_work_bytes", "zo_rms_norm_grad",
+    "zo_token_logprobs", "zo_token_logprobs_grad",
     "zo_ops_last_hip_error",
 )
 
@@ -74,6 +77,38 @@ class _Distill(ctypes.Structure):
                 ("row_weight", ctypes.c_void_p), ("tau", ctypes.c_float),
                 ("kd_weight", ctypes.c_float), ("ce_weight", ctypes.c_float),
                 ("loss", ctypes.c_void_p), ("dz", ctypes.c_void_p), ("lddz", ctypes.c_int64)]
+
+
+# Field types of the structs below: pointer, 32-bit and 64-bit integer, float.
+_FIELD = {"p": ctypes.c_void_p, "i": ctypes.c_int32, "l": ctypes.c_int64, "f": ctypes.c_float}
+
+
+def _fields(text):
+    return [(name, _FIELD[kind]) for name, kind in (w.split(":") for w in text.split())]
+
+
+class _I8(ctypes.Structure):
+    _fields_ = _fields("codes:p scales:p rows:l cols:l")
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = _fields("x:p dtype:i rows:l cols:l ldx:l residual:p ldr:l weight:p weight_dtype:i "
+                       "eps:f h:p ldh:l out:p ldo:l q:p rstd:p")
+
+
+class _NormBack(ctypes.Structure):
+    _fields_ = _fields("dy:p dtype:i rows:l cols:l lddy:l h:p ldh:l weight:p weight_dtype:i "
+                       "rstd:p dh:p lddh:l dx:p lddx:l dw:p work:p")
+
+
+class _Score(ctypes.Structure):
+    _fields_ = _fields("z:p dtype:i rows:l vocab:l ldz:l tokens:p tau:f logp:p stats:p top:i "
+                       "values:p columns:p")
+
+
+class _ScoreBack(ctypes.Structure):
+    _fields_ = _fields("z:p dtype:i rows:l vocab:l ldz:l tokens:p stats:p tau:f dlogp:p "
+                       "dentropy:p dz:p lddz:l")
 
 
 _lib = None
@@ -130,6 +165,17 @@ def lib():
             "zo_mx4_linear": ([vp, i32, i64, vp, vp, vp, i32, i64, vp], ci),
             "zo_top_logits": ([vp, i32, i64, i64, i64, i32, f32, vp, vp, vp, vp], ci),
             "zo_distill_loss": ([ctypes.POINTER(_Distill), vp], ci),
+            "zo_i8_code_bytes": ([i64, i64], i64),
+            "zo_i8_work_bytes": ([i64, i64], i64),
+            "zo_i8_quantize": ([vp, i32, i64, i64, i64, vp, vp, vp, vp], ci),
+            "zo_i8_dequantize": ([vp, vp, i32, i64, vp], ci),
+            "zo_i8_product": ([vp, vp, vp, i32, i64, vp], ci),
+            "zo_i8_linear": ([vp, i32, i64, vp, vp, vp, i32, i64, vp], ci),
+            "zo_rms_norm": ([ctypes.POINTER(_Norm), vp], ci),
+            "zo_rms_norm_work_bytes": ([i64, i64], i64),
+            "zo_rms_norm_grad": ([ctypes.POINTER(_NormBack), vp], ci),
+            "zo_token_logprobs": ([ctypes.POINTER(_Score), vp], ci),
+            "zo_token_logprobs_grad": ([ctypes.POINTER(_ScoreBack), vp], ci),
             "zo_ops_last_hip_error": ([], ctypes.c_char_p),
         }
         for name, (args, res) in sig.items():
@@ -508,6 +554,9 @@ class ZoAdam:
         return c.value
 
 
-from .operators import (Mx4, zo_distill_loss, zo_mx4_code_bytes, zo_mx4_dequantize,  # noqa: E402
-                        zo_mx4_linear, zo_mx4_product, zo_mx4_quantize, zo_mx4_scale_bytes,
-                        zo_top_logits)
+from .operators import (I8, Mx4, zo_distill_loss, zo_i8_code_bytes,  # noqa: E402
+                        zo_i8_dequantize, zo_i8_linear, zo_i8_product, zo_i8_quantize,
+                        zo_i8_work_bytes, zo_mx4_code_bytes, zo_mx4_dequantize, zo_mx4_linear,
+                        zo_mx4_product, zo_mx4_quantize, zo_mx4_scale_bytes, zo_rms_norm,
+                        zo_rms_norm_grad, zo_rms_norm_work_bytes, zo_token_logprobs,
+                        zo_token_logprobs_grad, zo_top_logits)

@@ -19,12 +19,16 @@ SOURCES = [os.path.join(CSRC, f) for f in ("zo_kernels.hip", "zo_server.hip",
                                            "zo_kernels_ua.hip", "zo_adam.cpp")]
 # the operators of zo_ops.h, apart from the optimizer step's kernels
 OPERATORS = [os.path.join(OPS, f) for f in ("zo_mx4_quant.hip", "zo_mx4_gemm.hip",
-                                            "zo_mx4_few.hip", "zo_top.hip", "zo_distill.hip",
+                                            "zo_mx4_few.hip", "zo_i8_quant.hip",
+                                            "zo_i8_gemm.hip", "zo_i8_few.hip", "zo_norm.hip",
+                                            "zo_top.hip", "zo_distill.hip", "zo_score.hip",
                                             "zo_ops.cpp")]
 HEADERS = [os.path.join(ROOT, "include", "zo_adam.h"), os.path.join(ROOT, "include", "zo_ops.h"),
            os.path.join(CSRC, "zo_internal.h"), os.path.join(CSRC, "zo_device.h"),
            os.path.join(CSRC, "zo_server.h"), os.path.join(OPS, "zo_ops_internal.h"),
-           os.path.join(OPS, "zo_ops_device.h"), os.path.join(OPS, "zo_mx4_device.h")]
+           os.path.join(OPS, "zo_ops_device.h"), os.path.join(OPS, "zo_mx4_device.h"),
+           os.path.join(OPS, "zo_tile_device.h"), os.path.join(OPS, "zo_i8_device.h"),
+           os.path.join(OPS, "zo_top_device.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-ffp-contract=off", "-fno-fast-math",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -49,7 +49,6 @@ __device__ __forceinline__ uint32_t convert2(uint32_t old, uint32_t w0, uint32_t
 }
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // acc += a-tile x b-tile; SA / SB: which byte of the scale dwords.
 template <int SA, int SB>
@@ -61,8 +60,6 @@ __device__ __forceinline__ f32x4 mfma(const u32x4 &a, const u32x4 &b, f32x4 acc,
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 4, 4, SA, (int)sa, SB,
                                                             (int)sb);
 }
-
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // The 32 x 32 x 64 form: lane l holds row l % 32, elements 32 (l / 32) .. + 31; of its
 // sixteen results lane l holds, for b's columns l % 32, a's rows

@@ -18,23 +18,6 @@ constexpr int kWaves = 8, kAhead = 8;
 // scale bytes beside the joined sums stay within 64 KiB.
 constexpr int kFusedTiles = 52;
 
-template <int GT>
-__device__ __forceinline__ void store_few(typename Elem<GT>::T *p, const f32x4 &v, int64_t nv)
-{
-    if (nv >= 4) {
-        if constexpr (GT == GT_F32) {
-            *reinterpret_cast<u32x4_a2 *>(p) = __builtin_bit_cast(u32x4, v);
-        } else {
-            const u32x2 w = {(uint32_t)narrow<GT>(v[0]) | (uint32_t)narrow<GT>(v[1]) << 16,
-                             (uint32_t)narrow<GT>(v[2]) | (uint32_t)narrow<GT>(v[3]) << 16};
-            *reinterpret_cast<u32x2_a2 *>(p) = w;
-        }
-    } else {
-        for (int q = 0; q < 4; ++q)
-            if (q < nv) p[q] = narrow<GT>(v[q]);
-    }
-}
-
 // The rows x (128 kt) activations in the operand's order: codes[t][lane], and a
 // scale byte for each.  One block of 32 per thread and turn; columns that are not there
 // are zeros, rows that are not there stay what they were: they reach no result.

@@ -14,6 +14,8 @@ namespace zo {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 // The same on any element boundary: one access each, the hardware splits it.
 typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
@@ -147,6 +149,24 @@ __device__ __forceinline__ u32x4 pack16(const float (&v)[Elem<GT>::kVec])
             w[q] = (uint32_t)narrow<GT>(v[2 * q]) | (uint32_t)narrow<GT>(v[2 * q + 1]) << 16;
     }
     return w;
+}
+
+// Stores the first nv of four floats, rounded.
+template <int GT>
+__device__ __forceinline__ void store_few(typename Elem<GT>::T *p, const f32x4 &v, int64_t nv)
+{
+    if (nv >= 4) {
+        if constexpr (GT == GT_F32) {
+            *reinterpret_cast<u32x4_a2 *>(p) = __builtin_bit_cast(u32x4, v);
+        } else {
+            const u32x2 w = {(uint32_t)narrow<GT>(v[0]) | (uint32_t)narrow<GT>(v[1]) << 16,
+                             (uint32_t)narrow<GT>(v[2]) | (uint32_t)narrow<GT>(v[3]) << 16};
+            *reinterpret_cast<u32x2_a2 *>(p) = w;
+        }
+    } else {
+        for (int q = 0; q < 4; ++q)
+            if (q < nv) p[q] = narrow<GT>(v[q]);
+    }
 }
 
 constexpr float kLog2e = 1.44269504088896340736f;

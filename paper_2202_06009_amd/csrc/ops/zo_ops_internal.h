@@ -45,6 +45,40 @@ bool few_fused(int64_t rows, int64_t n, int64_t k);
 hipError_t launch_mx4_few_fused(const void *x, int gx, int64_t rows, int64_t cols, int64_t ldx,
                                 const Mx4View &b, void *out, int gt, int64_t ld, hipStream_t st);
 
+// An i8 matrix as the kernels take it: rows of `wide` bytes.
+struct I8View {
+    int8_t *codes;
+    float *scales;
+    int64_t rows, cols, wide;
+};
+
+bool i8_quantize_fits(int64_t rows, int64_t cols, bool transposed);
+bool i8_product_fits(int64_t m, int64_t n, int64_t k);
+// Sets of partial column maxima that a quantisation along the columns leaves in its
+// workspace.
+int64_t i8_blocks(int64_t rows);
+
+hipError_t launch_i8_quantize(const void *x, int gt, int64_t rows, int64_t cols, int64_t ld,
+                              const I8View *q, const I8View *qt, uint32_t *work, hipStream_t st);
+hipError_t launch_i8_dequantize(const I8View &q, void *out, int gt, int64_t ld, hipStream_t st);
+hipError_t launch_i8_product(const I8View &a, const I8View &b, void *out, int gt, int64_t ld,
+                             hipStream_t st);
+// As for the 4-bit products.
+constexpr int kI8FewRows = 64;
+bool i8_few_fits(int64_t n, int64_t k);
+hipError_t launch_i8_few(const I8View &a, const I8View &b, void *out, int gt, int64_t ld,
+                         hipStream_t st);
+bool i8_few_fused(int64_t rows, int64_t n, int64_t k);
+hipError_t launch_i8_few_fused(const void *x, int gx, int64_t rows, int64_t cols, int64_t ldx,
+                               const I8View &b, void *out, int gt, int64_t ld, hipStream_t st);
+
+// Blocks of rows whose parts of dw a norm's backward pass leaves in its workspace.
+int64_t norm_grad_blocks(int64_t rows);
+hipError_t launch_norm(const zo_norm &a, const I8View &q, hipStream_t st);
+hipError_t launch_norm_grad(const zo_norm_back &a, hipStream_t st);
+hipError_t launch_score(const zo_score &a, hipStream_t st);
+hipError_t launch_score_grad(const zo_score_back &a, hipStream_t st);
+
 struct TopArgs {
     const void *z;
     int64_t rows, vocab, ld;

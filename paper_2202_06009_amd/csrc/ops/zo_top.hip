@@ -17,162 +17,20 @@
 // counted digit by digit from memory (select_row): exact for everything, several
 // reads, and equal logits meet in one counter.  4096 x 50257 bfloat16, 64 wanted: 142 us;
 // with a NaN in every row 1.3 ms, rows of one value or masked but for 40 columns 3.1 ms.
-#include "zo_ops_device.h"
+#include "zo_top_device.h"
 
 namespace zo {
 
-// Binary32 in the order of unsigned integers: ascending, -0 as +0, NaN last.
-__device__ __forceinline__ uint32_t order_key(float v)
-{
-    uint32_t b = __float_as_uint(v);
-    if (v == 0.0f) b = 0;
-    const uint32_t k = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-    return v != v ? 0xFFFFFFFFu : k;
-}
-
-__device__ __forceinline__ float key_value(uint32_t k)
-{
-    return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
-}
-
-__device__ __forceinline__ uint64_t full_key(uint32_t key, uint32_t column)
-{
-    return (uint64_t)key << 32 | (uint32_t)~column;
-}
-
-constexpr int kRoom = 2048;      // candidates
-
-template <int TH>
-struct TopShared {
-    alignas(16) uint64_t cand[kRoom];
-    uint32_t hist[256];
-    uint32_t sel[4];
-    uint32_t wcount[TH / 64];
-    float red[4][TH / 64];
+// Writes a row's result.
+struct PutLogit {
+    const TopArgs &a;
+    int64_t row;
+    __device__ __forceinline__ void operator()(int rank, uint64_t key) const
+    {
+        a.values[row * a.top + rank] = key_value((uint32_t)(key >> 32));
+        a.columns[row * a.top + rank] = (int32_t)~(uint32_t)key;
+    }
 };
-
-__device__ __forceinline__ void put_result(const TopArgs &a, int64_t row, int rank, uint64_t key)
-{
-    a.values[row * a.top + rank] = key_value((uint32_t)(key >> 32));
-    a.columns[row * a.top + rank] = (int32_t)~(uint32_t)key;
-}
-
-// The first a.top of the n keys in s.cand, in descending order, n <= kRoom.
-template <int TH>
-__device__ void sort_out(const TopArgs &a, int64_t row, TopShared<TH> &s, int n)
-{
-    const int tid = threadIdx.x;
-    if (n <= (TH < 384 ? TH : 384)) {
-        // each key's rank is the number of larger keys (all differ): no barriers; about
-        // as quick as the 45 steps below at 384 keys (280 keys: 208 us instead of 240
-        // for 256 of 4096 x 50257)
-        if (tid == 0 && (n & 1)) s.cand[n] = 0;
-        __syncthreads();
-        if (tid < n) {
-            const uint64_t mine = s.cand[tid];
-            const ulong2 *p = reinterpret_cast<const ulong2 *>(s.cand);
-            int rank = 0;
-            for (int j = 0; j < (n + 1) / 2; ++j) {
-                const ulong2 o = p[j];
-                rank += (o.x > mine) + (o.y > mine);
-            }
-            if (rank < a.top) put_result(a, row, rank, mine);
-        }
-        return;
-    }
-    // bitonic, descending, over the next power of two
-    int size = 512;
-    while (size < n) size *= 2;
-    for (int i = n + tid; i < size; i += TH) s.cand[i] = 0;
-    for (int k = 2; k <= size; k *= 2)
-        for (int j = k / 2; j; j /= 2) {
-            __syncthreads();
-            for (int t = tid; t < size / 2; t += TH) {
-                const int i = 2 * t - (t & (j - 1));      // bit j of i is 0
-                const uint64_t x = s.cand[i], y = s.cand[i + j];
-                if (((i & k) == 0) == (x < y)) {
-                    s.cand[i] = y;
-                    s.cand[i + j] = x;
-                }
-            }
-        }
-    __syncthreads();
-    for (int i = tid; i < a.top; i += TH) put_result(a, row, i, s.cand[i]);
-}
-
-// The digit of the `left`-th largest key in s.hist (256 bins): s.sel[0], what is
-// then left within it in s.sel[1], and how many are in and above it in s.sel[2].
-// By the first wave, four bins a lane.
-template <int TH>
-__device__ __forceinline__ void find_bin(TopShared<TH> &s, uint32_t left)
-{
-    const int lane = threadIdx.x;
-    if (lane >= 64) return;
-    const u32x4 h = *reinterpret_cast<const u32x4 *>(s.hist + 4 * lane);
-    const uint32_t own = h[0] + h[1] + h[2] + h[3];
-    uint32_t n = own;                                   // of this lane and those above
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const uint32_t up = __shfl_down(n, o, 64);
-        if (lane + o < 64) n += up;
-    }
-    uint32_t above = n - own;
-#pragma unroll
-    for (int q = 3; q >= 0; --q) {
-        if (above < left && above + h[q] >= left) {
-            s.sel[0] = 4 * lane + q;
-            s.sel[1] = left - above;
-            s.sel[2] = above + h[q];
-        }
-        above += h[q];
-    }
-}
-
-// Any row, from memory: the k-th largest key digit by digit, the keys above it
-// and the lowest columns of those equal to it.
-template <int GT, int TH>
-__device__ void select_row(const TopArgs &a, int64_t row, TopShared<TH> &s)
-{
-    constexpr int NW = TH / 64;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const auto *z = static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ld;
-    const int64_t V = a.vocab;
-    uint32_t prefix = 0, left = (uint32_t)a.top;
-    for (int p = 24; p >= 0; p -= 8) {
-        __syncthreads();
-        for (int i = tid; i < 256; i += TH) s.hist[i] = 0;
-        __syncthreads();
-        for (int64_t i = tid; i < V; i += TH) {
-            const uint32_t k = order_key(widen<GT>(z[i]));
-            if (((uint64_t)(k ^ prefix) >> (p + 8)) == 0) atomicAdd(&s.hist[k >> p & 255], 1u);
-        }
-        __syncthreads();
-        find_bin<TH>(s, left);
-        __syncthreads();
-        prefix |= s.sel[0] << p;
-        left = s.sel[1];
-    }
-    __syncthreads();
-    if (tid == 0) s.sel[0] = 0;
-    uint32_t equal = 0;                                  // so far
-    for (int64_t i0 = 0; i0 < V; i0 += TH) {
-        const int64_t i = i0 + tid;
-        const uint32_t k = i < V ? order_key(widen<GT>(z[i])) : 0;
-        const uint64_t mask = __ballot(i < V && k == prefix);
-        if (lane == 0) s.wcount[wave] = __popcll(mask);
-        __syncthreads();
-        if (i < V && k > prefix) s.cand[atomicAdd(&s.sel[0], 1u)] = full_key(k, (uint32_t)i);
-        uint32_t at = equal + __popcll(mask & ((1ull << lane) - 1));
-        for (int w = 0; w < NW; ++w) {
-            if (w < wave) at += s.wcount[w];
-            equal += s.wcount[w];
-        }
-        if (i < V && k == prefix && at < left)
-            s.cand[a.top - left + at] = full_key(k, (uint32_t)i);
-        __syncthreads();
-    }
-    sort_out<TH>(a, row, s, a.top);
-}
 
 // log(sum) from the pieces: largest logit m, s = sum of 2^(z c - r).
 __device__ __forceinline__ float lse_of(float m, float s, float tau, bool nan)
@@ -217,77 +75,6 @@ __device__ void lse_row(const TopArgs &a, int64_t row, TopShared<TH> &s)
     if (threadIdx.x == 0)
         a.lse[row] = lse_of(M, group_get<OpSum, TH / 64>(s.red[2]), a.tau,
                             group_get<OpMax, TH / 64>(s.red[1]) > 0.0f);
-}
-
-// Groups of the vectors of a thread, when more than a quarter as many logits are
-// wanted as there are threads.
-constexpr int kGroups = 4;
-
-// A thread's part in the bound: its largest logit, those of its groups, and which
-// of the groups have logits (bit g).
-struct GroupMaxima {
-    float all, of[kGroups];
-    uint32_t there;
-};
-
-// The key of a lower bound of the `top`-th largest logit from the group maxima, the
-// largest of which is M.  s.hist is zero.  Synchronises.
-template <int TH>
-__device__ __forceinline__ uint32_t find_bound(TopShared<TH> &s, uint32_t top, float M,
-                                               const GroupMaxima &m)
-{
-    constexpr int NW = TH / 64;
-    const int tid = threadIdx.x;
-    const bool by_thread = top <= TH / kGroups;
-    float lo = INFINITY;
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g)
-        if (m.there >> g & 1) lo = fminf(lo, m.of[g]);
-    if (by_thread) lo = m.there ? m.all : INFINITY;
-    group_put<OpMin>(lo, s.red[1]);
-    __syncthreads();
-    lo = group_get<OpMin, NW>(s.red[1]);
-    // bins of key - key(lo), shifted until 256 cover the range; a NaN falls in none
-    const uint32_t klo = order_key(lo);
-    const int shift = max(0, 24 - __clz((int)(order_key(M) - klo)));
-    const int fine = max(0, shift - 8);
-    auto count = [&](uint32_t from, int by, uint32_t bins) {
-        auto one = [&](float g, bool there) {
-            const uint32_t k = (order_key(g) - from) >> by;
-            if (there && k < bins) atomicAdd(&s.hist[k], 1u);
-        };
-        if (by_thread) {
-            one(m.all, m.there != 0);
-        } else {
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) one(m.of[g], m.there >> g & 1);
-        }
-    };
-    count(klo, shift, 256);
-    __syncthreads();
-    find_bin<TH>(s, top);
-    __syncthreads();
-    const uint32_t left = s.sel[1];
-    uint32_t least = klo + (s.sel[0] << shift);
-    if (shift > 0 && s.sel[2] > top + 64) {
-        __syncthreads();
-        for (int i = tid; i < 256; i += TH) s.hist[i] = 0;
-        __syncthreads();
-        count(least, fine, 1u << (shift - fine));
-        __syncthreads();
-        find_bin<TH>(s, left);
-        __syncthreads();
-        least += s.sel[0] << fine;
-    }
-    return least;
-}
-
-// A logit that reaches the bound joins the candidates, while there is room.
-template <int TH>
-__device__ __forceinline__ void offer(TopShared<TH> &s, float v, int64_t i)
-{
-    const uint32_t at = atomicAdd(&s.sel[3], 1u);
-    if (at < kRoom) s.cand[at] = full_key(order_key(v), (uint32_t)i);
 }
 
 // Rows that do not fit registers: the same with a second read of the row, the sums
@@ -339,7 +126,7 @@ __global__ __launch_bounds__(1024) void k_top_long(TopArgs a)
     const float total = group_get<OpSum, NW>(s.red[2]);
     if (total != total) {                                // NaN or an infinity is about
         if (a.lse) lse_row<GT, TH>(a, row, s);
-        select_row<GT, TH>(a, row, s);
+        select_row<GT, TH>(z, V, a.top, s, PutLogit{a, row});
         return;
     }
     if (a.lse && tid == 0) a.lse[row] = lse_of(M, total, a.tau, false);
@@ -357,9 +144,9 @@ __global__ __launch_bounds__(1024) void k_top_long(TopArgs a)
     __syncthreads();
     const uint32_t n = s.sel[3];
     if (n > kRoom)
-        select_row<GT, TH>(a, row, s);
+        select_row<GT, TH>(z, V, a.top, s, PutLogit{a, row});
     else
-        sort_out<TH>(a, row, s, (int)n);
+        sort_out<TH>(s, (int)n, a.top, PutLogit{a, row});
 }
 
 template <int GT, int TH, int NV>
@@ -370,7 +157,8 @@ __global__ __launch_bounds__(TH, TH == 768 ? 6 : 4) void k_top(TopArgs a)
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x, V = a.vocab;
     Resident<GT, TH, NV> x;
-    x.load(static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ld, V);
+    const auto *z = static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ld;
+    x.load(z, V);
     for (int i = tid; i < 256; i += TH) s.hist[i] = 0;
     if (tid == 0) s.sel[3] = 0;
 
@@ -428,8 +216,8 @@ __global__ __launch_bounds__(TH, TH == 768 ? 6 : 4) void k_top(TopArgs a)
             if (x.at(v) < x.vecs && (all || max_of<GT>(x.w[v]) >= bound)) {
 #pragma unroll
                 for (int q = 0; q < K; ++q) {
-                    const float z = elem_of<GT>(x.w[v], q);
-                    if (all || z >= bound) offer<TH>(s, z, x.at(v) * K + q);
+                    const float e = elem_of<GT>(x.w[v], q);
+                    if (all || e >= bound) offer<TH>(s, e, x.at(v) * K + q);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -438,9 +226,9 @@ __global__ __launch_bounds__(TH, TH == 768 ? 6 : 4) void k_top(TopArgs a)
         counted = s.sel[3] > kRoom;
     }
     if (counted)
-        select_row<GT, TH>(a, row, s);
+        select_row<GT, TH>(z, V, a.top, s, PutLogit{a, row});
     else
-        sort_out<TH>(a, row, s, (int)s.sel[3]);
+        sort_out<TH>(s, (int)s.sel[3], a.top, PutLogit{a, row});
     if (a.lse && !plain) lse_row<GT, TH>(a, row, s);     // the row's registers are free
 }
 

@@ -1,8 +1,9 @@
 """Python binding of the operators declared in ``include/zo_ops.h``.
 
 Argument marshalling only, with the C names: matrices in microscaled 4-bit
-floating point (``Mx4``) and their products, a teacher's top logits, the
-distillation loss with the gradient of the student's logits.  Device buffers
+floating point (``Mx4``) and in 8-bit integers (``I8``) and their products, the
+root-mean-square norm, a teacher's top logits, the distillation loss with the
+gradient of the student's logits, the log probabilities of tokens.  Device buffers
 are torch tensors; two-dimensional ones may have any row stride as long as
 their rows are contiguous.  Every call checks element types, shapes and
 devices before anything reaches the device and enqueues on ``stream`` (torch's
@@ -14,7 +15,8 @@ import ctypes
 
 import torch
 
-from . import ZoError, ZO_EHIP, ZO_EINVAL, ZO_OK, _Distill, _Mx4, lib
+from . import (ZoError, ZO_EHIP, ZO_EINVAL, ZO_OK, _Distill, _I8, _Mx4, _Norm, _NormBack, _Score,
+               _ScoreBack, lib)
 
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _MAX_DIM = 1 << 30
@@ -62,6 +64,48 @@ class Mx4:
             raise ValueError("codes, scales: expected tensors on one GPU")
         self.rows, self.cols, self.codes, self.scales, self.dev = rows, cols, codes, scales, dev
         self._c = _Mx4(codes.data_ptr(), scales.data_ptr(), rows, cols)
+        self._at = ctypes.addressof(self._c)
+
+
+def zo_i8_code_bytes(rows, cols):
+    """Bytes of the codes of a rows x cols 8-bit matrix."""
+    return _size(lib().zo_i8_code_bytes(int(rows), int(cols)), "zo_i8_code_bytes")
+
+
+def zo_i8_work_bytes(rows, cols):
+    """Bytes of the workspace in which zo_i8_quantize finds the largest magnitudes of the
+    columns of a rows x cols matrix."""
+    return _size(lib().zo_i8_work_bytes(int(rows), int(cols)), "zo_i8_work_bytes")
+
+
+class I8:
+    """A rows x cols matrix in 8-bit integers with a scale for each row: ``codes``, an
+    int8 device tensor of rows of cols rounded up to a multiple of 128 (zero beyond cols),
+    and ``scales``, float32 [rows] (allocated when not given).  Its rows are the axis that
+    products reduce over."""
+
+    __slots__ = ("rows", "cols", "codes", "scales", "dev", "_c", "_at")
+
+    def __init__(self, rows, cols, codes=None, scales=None, device="cuda"):
+        rows, cols = int(rows), int(cols)
+        if not (0 <= rows <= _MAX_DIM and 0 <= cols <= _MAX_DIM):
+            raise ZoError(ZO_EINVAL, "I8")
+        n = rows * ((cols + 127) >> 7 << 7)
+        if codes is None:
+            codes = torch.empty(n, dtype=torch.int8, device=device)
+        if scales is None:
+            scales = torch.empty(rows, dtype=torch.float32, device=codes.device)
+        if codes.dtype is not torch.int8 or scales.dtype is not torch.float32:
+            raise ValueError(f"codes, scales: expected int8 and float32, got {codes.dtype} and "
+                             f"{scales.dtype}")
+        for t, k, what in ((codes, n, "codes"), (scales, rows, "scales")):
+            if t.numel() < k or not t.is_contiguous():
+                raise ValueError(f"{what}: needs {k} contiguous elements, has {t.numel()}")
+        dev = codes.get_device()
+        if dev < 0 or scales.get_device() != dev:
+            raise ValueError("codes, scales: expected tensors on one GPU")
+        self.rows, self.cols, self.codes, self.scales, self.dev = rows, cols, codes, scales, dev
+        self._c = _I8(codes.data_ptr(), scales.data_ptr(), rows, cols)
         self._at = ctypes.addressof(self._c)
 
 
@@ -122,6 +166,40 @@ def _mx4(q, what, dev):
     return q._at
 
 
+def _i8(q, what, dev):
+    """Address of q's C struct."""
+    if type(q) is not I8:
+        raise ValueError(f"{what}: expected an I8")
+    if q.dev != dev:
+        raise ValueError(f"{what}: expected an I8 on GPU {dev}, got one on GPU {q.dev}")
+    return q._at
+
+
+def _same(t, what, dev, dtype, rows, cols):
+    """(pointer, row stride) of a matrix of this type and shape, or (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if t.dtype is not dtype:
+        raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
+    p, _, ld = _matrix(t, what, dev, rows, cols)
+    return p, ld
+
+
+def _weight(t, dev, dtype, cols):
+    """(pointer, element type) of a norm's weight."""
+    if t.dtype is not dtype and t.dtype is not torch.float32:
+        raise ValueError(f"weight: expected {dtype} or float32, got {t.dtype}")
+    return _vector(t, "weight", dev, t.dtype, (cols,)), _DTYPES[t.dtype]
+
+
+def _room(t, what, dev, size):
+    """Pointer of a workspace of at least `size` bytes."""
+    if not t.is_contiguous() or t.numel() * t.element_size() < size:
+        raise ValueError(f"{what}: needs {size} contiguous bytes, has "
+                         f"{t.numel() * t.element_size()}")
+    return _at(t, what, dev)
+
+
 _functions = {}
 
 
@@ -142,7 +220,7 @@ def _run(where, dev, stream, args, tensors):
     else:
         rc = f(*args, stream.cuda_stream)
         for t in tensors:
-            for x in ((t.codes, t.scales) if type(t) is Mx4 else (t,)):
+            for x in ((t.codes, t.scales) if type(t) in (Mx4, I8) else (t,)):
                 if x is not None:
                     x.record_stream(stream)
     if rc != ZO_OK:
@@ -236,3 +314,142 @@ def zo_distill_loss(z, values, columns, loss=None, dz=None, *, tau=1.0, teacher_
                  _vector(loss, "loss", dev, torch.float32, (rows,)), pdz, lddz)
     _run("zo_distill_loss", dev, stream, (ctypes.byref(a),),
          (z, values, columns, teacher_lse, labels, row_weight, loss, dz))
+
+
+def zo_i8_quantize(x, q=None, qt=None, work=None, stream=None):
+    """x [rows, cols] into q (an I8 of rows x cols, a scale for each of x's rows) and / or
+    qt (cols x rows, a scale for each of x's columns); qt needs work, a tensor of
+    zo_i8_work_bytes(rows, cols) bytes."""
+    dev = _device_of(x, "x")
+    p, dt, ld = _matrix(x, "x", dev)
+    rows, cols = x.shape
+    room = None
+    if qt is not None and rows and cols:
+        if work is None:
+            raise ValueError("work: needed with qt")
+        room = _room(work, "work", dev, lib().zo_i8_work_bytes(rows, cols))
+    _run("zo_i8_quantize", dev, stream,
+         (p, dt, rows, cols, ld, None if q is None else _i8(q, "q", dev),
+          None if qt is None else _i8(qt, "qt", dev), room), (x, q, qt, work))
+
+
+def zo_i8_dequantize(q, out, stream=None):
+    """The values of q into out [q.rows, q.cols]."""
+    dev = _device_of(out, "out")
+    pq = _i8(q, "q", dev)
+    p, dt, ld = _matrix(out, "out", dev, q.rows, q.cols)
+    _run("zo_i8_dequantize", dev, stream, (pq, p, dt, ld), (q, out))
+
+
+def zo_i8_product(a, b, out, stream=None):
+    """out [a.rows, b.rows] = a b^T, reduced over the columns of both (at most 131072)."""
+    dev = _device_of(out, "out")
+    pa, pb = _i8(a, "a", dev), _i8(b, "b", dev)
+    p, dt, ld = _matrix(out, "out", dev, a.rows, b.rows)
+    _run("zo_i8_product", dev, stream, (pa, pb, p, dt, ld), (a, b, out))
+
+
+def zo_i8_linear(x, w, out, xq, stream=None):
+    """out [rows, w.rows] = x quantised along its rows times w^T; xq (an I8 of x's shape)
+    is workspace."""
+    dev = _device_of(x, "x")
+    pw, pq = _i8(w, "w", dev), _i8(xq, "xq", dev)
+    px, dx, ldx = _matrix(x, "x", dev, xq.rows, xq.cols)
+    po, do, ldo = _matrix(out, "out", dev, xq.rows, w.rows)
+    _run("zo_i8_linear", dev, stream, (px, dx, ldx, pw, pq, po, do, ldo), (x, w, out, xq))
+
+
+def zo_rms_norm(x, weight, *, residual=None, h=None, out=None, q=None, rstd=None, eps=1e-5,
+                stream=None):
+    """h = x + residual (x [rows, cols]; without a residual x) and its root-mean-square norm
+    times weight (x's type or float32, [cols]): into out (x's type) and / or q (an I8 of
+    x's shape); 1 / sqrt(mean h^2 + eps) into rstd (float32 [rows]), which with h is what
+    the gradient needs.  h may be x or residual itself, and so may out where h is not."""
+    dev = _device_of(x, "x")
+    p, dt, ldx = _matrix(x, "x", dev)
+    rows, cols = x.shape
+    dtype = x.dtype
+    pr, ldr = _same(residual, "residual", dev, dtype, rows, cols)
+    pw, wt = _weight(weight, dev, dtype, cols)
+    ph, ldh = _same(h, "h", dev, dtype, rows, cols)
+    po, ldo = _same(out, "out", dev, dtype, rows, cols)
+    a = _Norm(p, dt, rows, cols, ldx, pr, ldr, pw, wt, float(eps), ph, ldh, po, ldo,
+              None if q is None else _i8(q, "q", dev),
+              _vector(rstd, "rstd", dev, torch.float32, (rows,)))
+    _run("zo_rms_norm", dev, stream, (ctypes.byref(a),), (x, residual, weight, h, out, q, rstd))
+
+
+def zo_rms_norm_work_bytes(rows, cols):
+    """Bytes of the workspace in which zo_rms_norm_grad sums the gradient of the weight."""
+    return _size(lib().zo_rms_norm_work_bytes(int(rows), int(cols)), "zo_rms_norm_work_bytes")
+
+
+def zo_rms_norm_grad(dy, h, weight, rstd, dx=None, dw=None, *, dh=None, work=None, stream=None):
+    """The gradients of zo_rms_norm from dy, that of out: dx (of x and of the residual; dh,
+    what reaches h past the norm, is added) and dw (float32 [cols]), which needs work, a
+    tensor of zo_rms_norm_work_bytes(rows, cols) bytes.  dx may be dy, h or dh itself."""
+    dev = _device_of(dy, "dy")
+    p, dt, lddy = _matrix(dy, "dy", dev)
+    rows, cols = dy.shape
+    dtype = dy.dtype
+    ph, ldh = _same(h, "h", dev, dtype, rows, cols)
+    pw, wt = _weight(weight, dev, dtype, cols)
+    po, lddh = _same(dh, "dh", dev, dtype, rows, cols)
+    px, lddx = _same(dx, "dx", dev, dtype, rows, cols)
+    room = None
+    if dw is not None and rows:
+        if work is None:
+            raise ValueError("work: needed with dw")
+        room = _room(work, "work", dev, lib().zo_rms_norm_work_bytes(rows, cols))
+    a = _NormBack(p, dt, rows, cols, lddy, ph, ldh, pw, wt,
+                  _vector(rstd, "rstd", dev, torch.float32, (rows,)), po, lddh, px, lddx,
+                  _vector(dw, "dw", dev, torch.float32, (cols,)), room)
+    _run("zo_rms_norm_grad", dev, stream, (ctypes.byref(a),),
+         (dy, h, weight, rstd, dh, dx, dw, work))
+
+
+def zo_token_logprobs(z, tokens=None, logp=None, stats=None, values=None, columns=None, *,
+                      tau=1.0, stream=None):
+    """Under softmax(z / tau) of every row of z [rows, vocab]: the log probability of the
+    row's token (tokens int32 [rows], outside the vocabulary: none) into logp (float32
+    [rows]); the largest logit, the logarithm of the sum of exponentials about it and the
+    entropy into stats (float32 [rows, 3]), which the gradient needs; the values.shape[1]
+    largest log probabilities in descending order into values (float32) and their columns
+    into columns (int32)."""
+    dev = _device_of(z, "z")
+    p, dt, ld = _matrix(z, "z", dev)
+    rows, vocab = z.shape
+    top = 0
+    if values is not None:
+        if values.dim() != 2 or columns is None:
+            raise ValueError("values, columns: expected two matrices")
+        top = values.shape[1]
+    elif columns is not None:
+        raise ValueError("values, columns: expected two matrices")
+    if (tokens is None) != (logp is None):
+        raise ValueError("tokens, logp: expected both or neither")
+    a = _Score(p, dt, rows, vocab, ld, _vector(tokens, "tokens", dev, torch.int32, (rows,)),
+               float(tau),
+               _vector(logp, "logp", dev, torch.float32, (rows,)),
+               _vector(stats, "stats", dev, torch.float32, (rows, 3)), top,
+               _vector(values, "values", dev, torch.float32, (rows, top)),
+               _vector(columns, "columns", dev, torch.int32, (rows, top)))
+    _run("zo_token_logprobs", dev, stream, (ctypes.byref(a),),
+         (z, tokens, logp, stats, values, columns))
+
+
+def zo_token_logprobs_grad(z, stats, dz, *, tokens=None, dlogp=None, dentropy=None, tau=1.0,
+                           stream=None):
+    """The gradient of z (z's type and shape; may be z itself) from those of the tokens'
+    log probabilities and / or of the entropies (float32 [rows]), with the stats of
+    zo_token_logprobs.  Rows in which both are 0 are not read."""
+    dev = _device_of(z, "z")
+    p, dt, ld = _matrix(z, "z", dev)
+    rows, vocab = z.shape
+    pd, ldd = _same(dz, "dz", dev, z.dtype, rows, vocab)
+    a = _ScoreBack(p, dt, rows, vocab, ld, _vector(tokens, "tokens", dev, torch.int32, (rows,)),
+                   _vector(stats, "stats", dev, torch.float32, (rows, 3)), float(tau),
+                   _vector(dlogp, "dlogp", dev, torch.float32, (rows,)),
+                   _vector(dentropy, "dentropy", dev, torch.float32, (rows,)), pd, ldd)
+    _run("zo_token_logprobs_grad", dev, stream, (ctypes.byref(a),),
+         (z, tokens, stats, dlogp, dentropy, dz))
