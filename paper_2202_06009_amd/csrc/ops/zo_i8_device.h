@@ -66,29 +66,34 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t *s)
 }
 
 // A row's step s = a / 127 (a: its largest magnitude, as bits), and how codes x / s are
-// formed: as x times the rounded inverse, which is within 2^-16 of the quotient, or,
-// where that is next to the border of two codes, by a division in 64 bits.  A quotient of
-// two 24-bit numbers that is not such a border itself is at least 2^-33 of it away, so the
-// rounded 64-bit quotient stands on the same side.  Steps below 2^-100, whose inverse may
-// pass binary32, take the division throughout.  inv = 0 makes every code 0, those of NaN
-// and infinity too.
+// formed: from x times an inverse a little above that of s and one a little below it.  Where
+// both round to the same whole number the quotient, which lies between, does too; where not,
+// it is near the border of two codes, and a division in 64 bits decides: a quotient of two
+// 24-bit numbers that is not such a border itself is at least 2^-33 of it away, so the rounded
+// 64-bit quotient stands on the same side.  Steps below 2^-100, whose inverse may pass
+// binary32, take the division throughout.  Where both inverses are 0 all codes are 0.
 struct Step {
-    float s, inv;
+    float s, above, below;
     bool far;
 };
 
-__device__ __forceinline__ Step step_of(uint32_t a)
-{
-    Step t;
-    t.s = a >= kInfBits ? NAN : __uint_as_float(a) / 127.0f;
-    t.far = t.s < 0x1p-100f && t.s > 0.0f;
-    t.inv = t.s >= 0x1p-100f ? 1.0f / t.s : 0.0f;
-    return t;
-}
-
 __device__ __forceinline__ Step step_from(float s)
 {
-    return {s, s >= 0x1p-100f ? 1.0f / s : 0.0f, s < 0x1p-100f && s > 0.0f};
+    // the instruction is within 2^-23
+    const float inv = s >= 0x1p-100f ? __builtin_amdgcn_rcpf(s) : 0.0f;
+    return {s, inv * (1.0f + 0x1p-22f), inv * (1.0f - 0x1p-22f), s < 0x1p-100f && s > 0.0f};
+}
+
+__device__ __forceinline__ Step step_of(uint32_t a)
+{
+    // a / 127 rounded to nearest: the quotient by the rounded inverse of 127, then its
+    // remainder, which is exact, by it again; a division where the quotient is near the
+    // numbers below the normal ones
+    constexpr float kInverse = 1.0f / 127.0f;
+    const float x = __uint_as_float(a), q = x * kInverse;
+    float s = __builtin_fmaf(__builtin_fmaf(-127.0f, q, x), kInverse, q);
+    if (a < 0x0E000000u) s = x / 127.0f;        // 2^-99
+    return step_from(a >= kInfBits ? NAN : s);
 }
 
 __device__ __forceinline__ int exact_code(float x, float s)
@@ -97,30 +102,27 @@ __device__ __forceinline__ int exact_code(float x, float s)
     return (int)fmin(fmax(q, -127.0), 127.0);
 }
 
-// Whether a quotient is within 2^-13 of a border.
-__device__ __forceinline__ bool near_border(float r, float rounded)
+// The last bytes of x inv + 1.5 * 2^23, which rounds x inv to a whole number, to nearest even.
+__device__ __forceinline__ uint32_t rounded4(const float (&x)[4], float inv)
 {
-    return fabsf(r - rounded) > 0.5f - 0x1p-13f;
+    uint32_t n[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) n[q] = __float_as_uint(__builtin_fmaf(x[q], inv, 0x1.8p23f));
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(n[3], n[2], 0x0C0C0400u),
+                                 __builtin_amdgcn_perm(n[1], n[0], 0x0C0C0400u), 0x05040100u);
 }
 
 // The codes of four values in a dword, the first lowest.
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, const Step &t)
 {
     const float x[4] = {a, b, c, d};
-    uint32_t w = 0;
-    bool hard = t.far;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const float r = x[q] * t.inv, f = __builtin_rintf(r);
-        hard |= near_border(r, f);
-        w |= ((uint32_t)(int)f & 255u) << (8 * q);
-    }
-    if (hard) {
+    uint32_t w = rounded4(x, t.above);
+    if (w != rounded4(x, t.below) || t.far) {
         w = 0;
 #pragma unroll
         for (int q = 0; q < 4; ++q) w |= ((uint32_t)exact_code(x[q], t.s) & 255u) << (8 * q);
     }
-    return w;
+    return t.above == 0.0f && !t.far ? 0u : w;
 }
 
 // The codes of a vector's elements, at p (kVec bytes, aligned to them).
@@ -132,6 +134,39 @@ __device__ __forceinline__ void store_codes(int8_t *p, const float (&x)[K], cons
         *reinterpret_cast<u32x2 *>(p) = u32x2{lo, codes4(x[4], x[5], x[6], x[7], t)};
     else
         *reinterpret_cast<uint32_t *>(p) = lo;
+}
+
+// Thread t's vectors t, t + TH, ... of a row of `cols` elements; what is not there is 0, or
+// not stored.  Whole vectors first, so that all their loads are under way together.
+template <int GT, int TH, int NV>
+__device__ __forceinline__ void load_row(u32x4 (&w)[NV], const typename Elem<GT>::T *p, int cols,
+                                         int t)
+{
+    constexpr int K = Elem<GT>::kVec;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int c = (v * TH + t) * K;
+        w[v] = u32x4{0, 0, 0, 0};
+        if (c + K <= cols) w[v] = *reinterpret_cast<const u32x4_a2 *>(p + c);
+    }
+    if (cols % K)
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * TH + t) * K;
+            if (c < cols && c + K > cols) w[v] = load16<GT>(p + c, cols - c);
+        }
+}
+
+// Stores vector v of the row.
+template <int GT>
+__device__ __forceinline__ void store_vector(typename Elem<GT>::T *p, const u32x4 &w, int c,
+                                             int cols)
+{
+    constexpr int K = Elem<GT>::kVec;
+    if (c + K <= cols)
+        *reinterpret_cast<u32x4_a2 *>(p + c) = w;
+    else if (c < cols)
+        store16<GT>(p + c, w, cols - c);
 }
 
 // Largest magnitudes of packed elements, element by element, in their own type.

@@ -4,6 +4,9 @@
 
 namespace zo {
 
+template <int N>
+using Int = std::integral_constant<int, N>;
+
 // Rows of a workgroup where the columns' maxima are wanted too.  One set of partial maxima
 // for that many rows goes to memory: 4 bytes for 16 or more elements.
 static int64_t rows_a_block(int64_t rows)
@@ -18,30 +21,28 @@ int64_t i8_blocks(int64_t rows)
     return (rows + per - 1) / per;
 }
 
-// Rows [blockIdx.x * per, + per), by teams of TH threads that hold a row in NV vectors a
-// thread.  q.codes: NULL, or the rows' codes.  COLS: the columns' largest magnitudes over
-// these rows into work[blockIdx.x][cols].
-template <int GT, int TH, int NV, bool COLS>
-__global__ __launch_bounds__(TH < 256 ? 256 : TH) void k_i8_rows(
-    const typename Elem<GT>::T *__restrict__ x, int64_t rows, int64_t cols, int64_t ld, I8View q,
-    uint32_t *__restrict__ work, int64_t per)
+// Rows [blockIdx.x * per, + per), by TEAMS teams of TH threads that hold a row in NV vectors
+// a thread, the next row on its way.  q.codes: NULL, or the rows' codes.  COLS: the columns'
+// largest magnitudes over these rows into work[blockIdx.x][cols].
+template <int GT, int TH, int NV, int TEAMS, bool COLS>
+__global__ __launch_bounds__(TH *TEAMS, COLS && NV <= 2 ? 8 : 4) void k_i8_rows(
+    const typename Elem<GT>::T *__restrict__ x, int64_t rows, int cols, int64_t ld, I8View q,
+    uint32_t *__restrict__ work, int per)
 {
-    constexpr int K = Elem<GT>::kVec, TEAMS = TH < 256 ? 256 / TH : 1, NW = TH / 64;
-    __shared__ uint32_t red[2][NW];
-    __shared__ u32x4 joined[COLS && TEAMS > 1 ? TEAMS * TH * NV : 1];
-    const int t = threadIdx.x % TH, team = TEAMS > 1 ? threadIdx.x / TH : 0;
-    const int64_t from = blockIdx.x * per, to = min(rows, from + per);
-    u32x4 most[COLS ? NV : 1] = {};
-    int turn = 0;
-    for (int64_t r = from + team; r < to; r += TEAMS, turn ^= 1) {
-        const typename Elem<GT>::T *p = x + r * ld;
-        u32x4 w[NV];
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int64_t c = (int64_t)(v * TH + t) * K;
-            w[v] = u32x4{0, 0, 0, 0};
-            if (c < cols) w[v] = load16<GT>(p + c, cols - c);
-        }
+    constexpr int K = Elem<GT>::kVec, NW = TH / 64;
+    __shared__ uint32_t red[2][TEAMS][NW];
+    __shared__ u32x4 joined[COLS && TEAMS > 1 ? (TEAMS - 1) * TH * NV : 1];
+    const int t = threadIdx.x % TH, team = threadIdx.x / TH;
+    const int64_t from = (int64_t)blockIdx.x * per, to = min(rows, from + per);
+    const int turns = (int)(to - from + TEAMS - 1) / TEAMS;
+    u32x4 most[COLS ? NV : 1] = {}, w[NV];
+    // a team without a row takes the last one again, and stores no codes of it
+    auto fetch = [&](int turn) {
+        load_row<GT, TH>(w, x + min(from + turn * TEAMS + team, to - 1) * ld, cols, t);
+    };
+    fetch(0);
+    for (int turn = 0; turn < turns; ++turn) {
+        const int64_t r = from + turn * TEAMS + team;
         u32x4 m = {};
 #pragma unroll
         for (int v = 0; v < NV; ++v)
@@ -50,37 +51,56 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void k_i8_rows(
                 m[i] = packed_max<GT>(m[i], w[v][i]);
                 if constexpr (COLS) most[v][i] = packed_max<GT>(most[v][i], w[v][i]);
             }
-        if (!q.codes) continue;                  // the same for all
-        const Step s = step_of(row_max<TH>(max_in<GT>(m), red[turn]));
-        if (t == 0) q.scales[r] = s.s;
-        int8_t *to_codes = q.codes + r * q.wide;
+        if (!q.codes) {                          // the same for all
+            if (turn + 1 < turns) fetch(turn + 1);
+            continue;
+        }
+        uint32_t top = wave_max(max_in<GT>(m));
+        if constexpr (TH > 64) {
+            uint32_t *s = red[turn & 1][team];
+            if ((t & 63) == 0) s[t >> 6] = top;
+            __syncthreads();
+            top = s[0];
+#pragma unroll
+            for (int i = 1; i < NW; ++i) top = max(top, s[i]);
+        }
+        const Step s = step_of(top);
+        if (t == 0 && r < to) q.scales[r] = s.s;
+        int8_t *codes = q.codes + r * q.wide;
+        const int wide = r < to ? (int)q.wide : 0;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int64_t c = (int64_t)(v * TH + t) * K;
+            const int c = (v * TH + t) * K;
             float e[K];
+            repack<GT>(w[v]);
 #pragma unroll
             for (int i = 0; i < K; ++i) e[i] = elem_of<GT>(w[v], i);
-            if (c < q.wide) store_codes<K>(to_codes + c, e, s);
+            if (c < wide) store_codes<K>(codes + c, e, s);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        if (turn + 1 < turns) fetch(turn + 1);
     }
     if constexpr (COLS) {
         if constexpr (TEAMS > 1) {
+            if (team > 0)
 #pragma unroll
-            for (int v = 0; v < NV; ++v) joined[(team * NV + v) * TH + t] = most[v];
+                for (int v = 0; v < NV; ++v) joined[((team - 1) * NV + v) * TH + t] = most[v];
             __syncthreads();
             if (team > 0) return;
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
-                for (int k = 1; k < TEAMS; ++k) {
+            for (int v = 0; v < NV; ++v) {
+#pragma unroll 1
+                for (int k = 0; k < TEAMS - 1; ++k) {
                     const u32x4 o = joined[(k * NV + v) * TH + t];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) most[v][i] = packed_max<GT>(most[v][i], o[i]);
                 }
+            }
         }
-        uint32_t *to_work = work + blockIdx.x * cols;
+        uint32_t *to_work = work + (int64_t)blockIdx.x * cols;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int64_t c = (int64_t)(v * TH + t) * K;
+            const int c = (v * TH + t) * K;
 #pragma unroll
             for (int i = 0; i < K; ++i)
                 if (c + i < cols) to_work[c + i] = mag_bits(elem_of<GT>(most[v], i));
@@ -171,8 +191,7 @@ __global__ __launch_bounds__(256) void k_i8_cols(const typename Elem<GT>::T *__r
 {
     constexpr int K = Elem<GT>::kVec, LANES = 64 / K, GROUPS = 256 / LANES;
     __shared__ uint32_t tile[64][33];
-    const int64_t r0 = (int64_t)(blockIdx.x / strips) * 128;
-    const int64_t c0 = (int64_t)(blockIdx.x % strips) * 64;
+    const int64_t r0 = (int64_t)(blockIdx.x / strips) * 128, c0 = (int64_t)(blockIdx.x % strips) * 64;
     const int j = threadIdx.x % LANES, g = threadIdx.x / LANES;
     const int64_t c = c0 + j * K;
     Step s[K];
@@ -194,12 +213,14 @@ __global__ __launch_bounds__(256) void k_i8_cols(const typename Elem<GT>::T *__r
                                            elem_of<GT>(w[2], q), elem_of<GT>(w[3], q), s[q]);
     }
     __syncthreads();
+    // whole lines, past the caches (8192 x 6400 bfloat16 both ways 83.6 us, 82.6 so)
     const int i = threadIdx.x & 31;
 #pragma unroll
     for (int n = 0; n < 8; ++n) {
         const int k = n * 8 + (threadIdx.x >> 5);
         if (c0 + k < cols)
-            *reinterpret_cast<uint32_t *>(qt.codes + (c0 + k) * qt.wide + r0 + i * 4) = tile[k][i];
+            __builtin_nontemporal_store(
+                tile[k][i], reinterpret_cast<uint32_t *>(qt.codes + (c0 + k) * qt.wide + r0 + i * 4));
     }
 }
 
@@ -228,9 +249,9 @@ __global__ __launch_bounds__(256) void k_i8_dequantize(I8View q,
     }
 }
 
-// Columns that a workgroup's registers hold.
-template <int GT>
-constexpr int64_t kResident = 1024 * 8 * Elem<GT>::kVec;
+// Columns that a workgroup's registers hold, and with the columns' maxima.
+template <int GT, bool COLS>
+constexpr int64_t kResident = 1024 * (COLS ? 4 : 8) * Elem<GT>::kVec;
 
 static int64_t runs_of(int64_t cols, int64_t run) { return (cols + run - 1) / run; }
 
@@ -245,13 +266,15 @@ static hipError_t launch_rows(const typename Elem<GT>::T *x, int64_t rows, int64
                               int64_t ld, const I8View &q, uint32_t *work, hipStream_t st)
 {
     const int64_t vecs = (cols + 127) / 128 * (128 / Elem<GT>::kVec);
-    auto go = [&](auto th, auto nv) {
+    // threads of a row, their vectors, and rows at a time: where the columns are wanted, as
+    // many as a workgroup takes
+    auto go = [&](auto th, auto nv, auto teams) {
         constexpr int TH = decltype(th)::value, NV = decltype(nv)::value;
-        constexpr int TEAMS = TH < 256 ? 256 / TH : 1;
-        constexpr int THREADS = TH < 256 ? 256 : TH;
+        constexpr int TEAMS = COLS ? decltype(teams)::value : TH == 64 ? 4 : 1;
+        const auto kernel = k_i8_rows<GT, TH, NV, TEAMS, COLS>;
         if constexpr (COLS) {
-            return start(k_i8_rows<GT, TH, NV, true>, i8_blocks(rows), THREADS, 0, st, x, rows,
-                         cols, ld, q, work, rows_a_block(rows));
+            return start(kernel, i8_blocks(rows), TH * TEAMS, 0, st, x, rows, (int)cols, ld, q,
+                         work, (int)rows_a_block(rows));
         } else {
             hipError_t e = hipSuccess;
             for (int64_t r = 0; r < rows && e == hipSuccess; r += kLaunchRows) {
@@ -259,19 +282,23 @@ static hipError_t launch_rows(const typename Elem<GT>::T *x, int64_t rows, int64
                 I8View to = q;
                 to.codes += r * q.wide;
                 to.scales += r;
-                e = start(k_i8_rows<GT, TH, NV, false>, runs_of(part, TEAMS), THREADS, 0, st,
-                          x + r * ld, part, cols, ld, to, nullptr, TEAMS);
+                e = start(kernel, runs_of(part, TEAMS), TH * TEAMS, 0, st, x + r * ld, part,
+                          (int)cols, ld, to, nullptr, TEAMS);
             }
             return e;
         }
     };
-    using std::integral_constant;
-    if (vecs <= 64) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-    if (vecs <= 256) return go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
-    if (vecs <= 512) return go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-    if (vecs <= 1024) return go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
-    if (vecs <= 4096) return go(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
-    return go(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
+    if (vecs <= 64) return go(Int<64>{}, Int<1>{}, Int<16>{});
+    if (!COLS && vecs > 512 && vecs <= 1024) return go(Int<256>{}, Int<4>{}, Int<8>{});
+    if (vecs <= 256) return go(Int<128>{}, Int<2>{}, Int<8>{});
+    if (vecs <= 512) return go(Int<256>{}, Int<2>{}, Int<4>{});
+    if (vecs <= 1024) return go(Int<512>{}, Int<2>{}, Int<2>{});
+    if (vecs <= 2048) return go(Int<1024>{}, Int<2>{}, Int<1>{});
+    if (vecs <= 4096) return go(Int<1024>{}, Int<4>{}, Int<1>{});
+    if constexpr (COLS)
+        return hipErrorInvalidValue;            // the caller takes the long form
+    else
+        return go(Int<1024>{}, Int<8>{}, Int<1>{});
 }
 
 hipError_t launch_i8_quantize(const void *px, int gt, int64_t rows, int64_t cols, int64_t ld,
@@ -283,17 +310,20 @@ hipError_t launch_i8_quantize(const void *px, int gt, int64_t rows, int64_t cols
         const auto *x = static_cast<const typename Elem<GT>::T *>(px);
         const I8View none = {};
         hipError_t e = hipSuccess;
-        if (cols <= kResident<GT>) {
-            e = qt ? launch_rows<GT, true>(x, rows, cols, ld, q ? *q : none, work, st)
-                   : launch_rows<GT, false>(x, rows, cols, ld, *q, nullptr, st);
+        const bool joint = qt && cols <= kResident<GT, true>;
+        if (joint) {
+            e = launch_rows<GT, true>(x, rows, cols, ld, q ? *q : none, work, st);
         } else {
-            for (int64_t r = 0; q && r < rows && e == hipSuccess; r += kLaunchRows) {
-                I8View to = *q;
-                to.codes += r * q->wide;
-                to.scales += r;
-                e = start(k_i8_rows_long<GT>, rows - r < kLaunchRows ? rows - r : kLaunchRows,
-                          1024, 0, st, x + r * ld, cols, ld, to);
-            }
+            if (q && cols <= kResident<GT, false>)
+                e = launch_rows<GT, false>(x, rows, cols, ld, *q, nullptr, st);
+            else
+                for (int64_t r = 0; q && r < rows && e == hipSuccess; r += kLaunchRows) {
+                    I8View to = *q;
+                    to.codes += r * q->wide;
+                    to.scales += r;
+                    e = start(k_i8_rows_long<GT>, rows - r < kLaunchRows ? rows - r : kLaunchRows,
+                              1024, 0, st, x + r * ld, cols, ld, to);
+                }
             if (qt && e == hipSuccess) {
                 const int64_t all = runs_of(cols, 256 * K), runs = all < 1024 ? all : 1024;
                 e = start(k_i8_colmax<GT>, i8_blocks(rows) * runs, 256, 0, st, x, rows, cols, ld,
