@@ -245,13 +245,6 @@ __global__ __launch_bounds__(512, 2) void k_mx4_product_large(
     }
 }
 
-// Shared memory beyond 64 KiB has to be asked for.
-static hipError_t allow_lds(const void *kernel, uint32_t lds)
-{
-    if (lds <= 65536) return hipSuccess;
-    return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-}
-
 template <int GT, int MT, int NT, int WN, bool STREAM>
 static hipError_t launch_tiles(const Mx4View &a, const Mx4View &b, void *out, int64_t ld,
                                hipStream_t st)

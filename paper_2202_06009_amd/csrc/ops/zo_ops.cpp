@@ -290,7 +290,7 @@ int zo_i8_linear(const void *x, int32_t dtype, int64_t ldx, const zo_i8 *w, cons
     if (!zo::i8_product_fits(xq->rows, w->rows, w->cols)) return ZO_EINVAL;
     if (xq->rows == 0 || w->rows == 0) return ZO_OK;
     const zo::I8View v = view(xq);
-    if (zo::i8_few_fused(v.rows, w->rows, v.cols))
+    if (zo::i8_few_fused(v.rows, v.cols))
         return from_hip(zo::launch_i8_few_fused(x, gx, v.rows, v.cols, ldx, view(w), out, go, ldo,
                                                 stream));
     rc = from_hip(zo::launch_i8_quantize(x, gx, v.rows, v.cols, ldx, &v, nullptr, nullptr, stream));

@@ -59,6 +59,13 @@ static hipError_t start(void (*kernel)(P...), int64_t groups, int threads, uint3
                            dim3((uint32_t)threads), at, lds, st);
 }
 
+// Shared memory beyond 64 KiB has to be asked for.
+[[maybe_unused]] static hipError_t allow_lds(const void *kernel, uint32_t lds)
+{
+    if (lds <= 65536) return hipSuccess;
+    return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+}
+
 template <int GT>
 __device__ __forceinline__ float widen(typename Elem<GT>::T bits)
 {

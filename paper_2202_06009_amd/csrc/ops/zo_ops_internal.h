@@ -63,12 +63,14 @@ hipError_t launch_i8_quantize(const void *x, int gt, int64_t rows, int64_t cols,
 hipError_t launch_i8_dequantize(const I8View &q, void *out, int gt, int64_t ld, hipStream_t st);
 hipError_t launch_i8_product(const I8View &a, const I8View &b, void *out, int gt, int64_t ld,
                              hipStream_t st);
-// As for the 4-bit products.
-constexpr int kI8FewRows = 64;
+// As for the 4-bit products.  Few rows / tiles, us (rows x matrix): 32 x 6400 x 1600 6.6 / 7.0,
+// 40 8.0 / 7.1; 32 x 50257 x 1600 19.9 / 18.8, 40 21.4 / 18.9; 32 x 1600 x 6400 10.8 / 16.3, 40
+// 14.1 / 16.3, 64 17.0 / 16.6; 16 x 4096 x 1024 3.6 / 5.0, 40 5.2 / 5.0.
+constexpr int kI8FewRows = 32;
 bool i8_few_fits(int64_t n, int64_t k);
 hipError_t launch_i8_few(const I8View &a, const I8View &b, void *out, int gt, int64_t ld,
                          hipStream_t st);
-bool i8_few_fused(int64_t rows, int64_t n, int64_t k);
+bool i8_few_fused(int64_t rows, int64_t k);
 hipError_t launch_i8_few_fused(const void *x, int gx, int64_t rows, int64_t cols, int64_t ldx,
                                const I8View &b, void *out, int gt, int64_t ld, hipStream_t st);
 
