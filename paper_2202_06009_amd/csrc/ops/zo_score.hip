@@ -3,12 +3,9 @@
 //
 // With m the row's largest logit, t = (z - m) log2(e) / tau and e = 2^t:
 //   S = sum e, U = sum e t; log p = (z - m) / tau - ln S, entropy = ln S - ln 2 U / S.
-// The difference comes first, so that logits of any size keep their distances.  Terms of
-// t below kLeast add nothing to either sum (2^t is 0), so t is clamped there in U and
-// logits of -infinity need no case of their own.
+// A logit of -infinity adds nothing to either sum: where the product of 0 and -infinity has
+// made U a NaN, the vector is taken again with t clamped to kLeast.
 //
-// One workgroup per row; the bound is reading the logits once (k_score: the row stays in
-// registers).  The alternatives are found as zo_top.hip finds them.
 #include "zo_top_device.h"
 
 namespace zo {
@@ -46,6 +43,41 @@ __device__ __forceinline__ RowScore row_score(float m, float s, float u)
     return {m, log_s, fmaxf(log_s - kLn2 * (u / s), 0.0f)};
 }
 
+// Largest of a vector's elements: 16-bit ones two at a time by their bits, whose order as
+// signed integers is that of the numbers where the result is positive, and as unsigned ones the
+// opposite among negative numbers.  NaN passes as any
+// number: a row with one is not told from these.
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(i16x2, a),
+                                                                  __builtin_bit_cast(i16x2, b)));
+}
+
+__device__ __forceinline__ uint32_t pk_least(uint32_t a, uint32_t b)
+{
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, a),
+                                                                  __builtin_bit_cast(u16x2, b)));
+}
+
+template <int GT>
+__device__ __forceinline__ float largest_of(const u32x4 &w)
+{
+    if constexpr (GT == GT_F32) {
+        return max_of<GT>(w);
+    } else {
+        uint32_t m = pk_max(pk_max(w[0], w[1]), pk_max(w[2], w[3]));
+        m = pk_max(m, m >> 16);
+        if (m & 0x8000u) {
+            m = pk_least(pk_least(w[0], w[1]), pk_least(w[2], w[3]));
+            m = pk_least(m, m >> 16);
+        }
+        return widen<GT>((uint16_t)m);
+    }
+}
+
 // The row's token, or -1, and its logit.
 struct Token {
     int32_t at;
@@ -80,79 +112,146 @@ __device__ __forceinline__ void add_term(float z, float b, float c, float &s, fl
     u = __builtin_fmaf(e, fmaxf(t, kLeast), u);
 }
 
-template <int GT, int TH, int NV>
-__global__ __launch_bounds__(TH, TH == 768 ? 6 : 4) void k_score(zo_score a)
+// A vector's terms about b.
+template <int GT>
+__device__ __forceinline__ void add_vector(const u32x4 &w, float b, float c, float &s, float &u)
 {
-    constexpr int K = Elem<GT>::kVec, NW = TH / 64;
+    const float s0 = s, u0 = u;
+#pragma unroll
+    for (int q = 0; q < Elem<GT>::kVec; ++q) {
+        const float t = (elem_of<GT>(w, q) - b) * c, e = exp2_hw(t);
+        s += e;
+        u = __builtin_fmaf(e, t, u);
+    }
+    if (u != u) {
+        s = s0;
+        u = u0;
+#pragma unroll
+        for (int q = 0; q < Elem<GT>::kVec; ++q) add_term(elem_of<GT>(w, q), b, c, s, u);
+    }
+}
+
+// The sums about a larger logit than they were; from -infinity they are 0, or a NaN.
+__device__ __forceinline__ void move_base(float from, float to, float c, float &s, float &u)
+{
+    if (from == -INFINITY) return;
+    const float d = fmaxf((from - to) * c, kLeast), f = exp2_hw(d);
+    u = f * __builtin_fmaf(s, d, u);
+    s *= f;
+}
+
+// A row by TH threads, in one read.  The sums are those of 1024 lanes, of which a thread is
+// one, two or four: lane l takes the vectors l, l + 1024, ... of the row and sums about the
+// largest logit of its first, moved only when one is 2^64 times as likely; the sums of waves of
+// 64 lanes are joined in order.  So a row's results
+// are the same bits however many rows there are and whatever else is wanted.
+//
+// Every N-th of a lane's vectors belongs to the same group, four groups a thread.  The groups' maxima bound the k-th
+// largest logit from below, and only those that reach the bound, few more than are wanted, are
+// read again for the candidates.
+//
+// Nothing of the row stays in the registers, so that a CU has 2048 threads with several loads
+// each under way: 4096 x 50304 bfloat16 without alternatives 81 us, with 20 104; with the row in
+// registers, two workgroups of 768 threads a CU, 95 and 126.  Bound by vector instructions and
+// memory alike: the floor of one read is 64.
+template <int GT, int TH>
+__global__ __launch_bounds__(TH, 8) void k_score(zo_score a)
+{
+    constexpr int LANES = 1024 / TH, NW = TH / 64, K = Elem<GT>::kVec, G = kGroups, N = G / LANES;
     __shared__ TopShared<TH> sh;
-    __shared__ float more[NW];
+    __shared__ float red[2][16];
     const int tid = threadIdx.x;
-    const int64_t row = blockIdx.x, V = a.vocab;
+    const int vecs = (int)(a.vocab / K);
+    const int64_t row = blockIdx.x, V = a.vocab, whole = (int64_t)vecs * K;
     const auto *z = static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ldz;
     const Token token = read_token<GT>(a, row, z);
-    Resident<GT, TH, NV> x;
-    x.load(z, V);
+    const float c = log2_factor(a.tau);
+    GroupMaxima m = {-INFINITY, {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, 0};
+    float base[LANES], s[LANES] = {}, u[LANES] = {};
+    const float slack = fminf(64.0f / c, 0x1.fffffep127f);
+#pragma unroll
+    for (int l = 0; l < LANES; ++l) base[l] = -INFINITY;
+    for (int j = 0; j < vecs; j += 1024 * N) {
+        u32x4 w[N][LANES];
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int l = 0; l < LANES; ++l) {
+                // without a condition, past the end the last vector: behind a branch each load
+                // would wait for the one before
+                const int i = min(j + n * 1024 + l * TH + tid, vecs - 1);
+                w[n][l] = *reinterpret_cast<const u32x4_a2 *>(z + (int64_t)i * K);
+            }
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int l = 0; l < LANES; ++l)
+                if (j + n * 1024 + l * TH + tid < vecs) {
+                    const int g = n * LANES + l;
+                    const float top = largest_of<GT>(w[n][l]);
+                    m.of[g] = fmaxf(m.of[g], top);
+                    m.there |= 1u << g;
+                    if (top > base[l] + slack) {
+                        move_base(base[l], top, c, s[l], u[l]);
+                        base[l] = top;
+                    }
+                    add_vector<GT>(w[n][l], base[l] == -INFINITY ? 0.0f : base[l], c, s[l], u[l]);
+                }
+    }
+    // one each of the V % K logits that are left
+    const bool has_last = whole + tid < V;
+    const float last = has_last ? widen<GT>(z[whole + tid]) : -INFINITY;
+    if (has_last) {
+        if (last > base[0] + slack) {
+            move_base(base[0], last, c, s[0], u[0]);
+            base[0] = last;
+        }
+        add_term(last, base[0] == -INFINITY ? 0.0f : base[0], c, s[0], u[0]);
+    }
     for (int i = tid; i < 256; i += TH) sh.hist[i] = 0;
     if (tid == 0) sh.sel[3] = 0;
-
-    GroupMaxima m = {x.last, {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, 0};
+    m.all = last;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        if (v * TH < x.vecs)                             // the same for all threads
-            m.of[v % kGroups] = fmaxf(m.of[v % kGroups], max_of<GT>(x.w[v]));
-        __builtin_amdgcn_sched_barrier(0);
-    }
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-        m.all = fmaxf(m.all, m.of[g]);
-        if (x.at(g) < x.vecs) m.there |= 1u << g;
-    }
+    for (int g = 0; g < G; ++g) m.all = fmaxf(m.all, m.of[g]);
     group_put<OpMax>(m.all, sh.red[0]);
     __syncthreads();
-    const float M = group_get<OpMax, NW>(sh.red[0]), b = M == -INFINITY ? 0.0f : M;
-    const float c = log2_factor(a.tau);
-    float s = 0.0f, u = 0.0f;
-    add_term(x.last, b, c, s, u);
+    const float M = group_get<OpMax, NW>(sh.red[0]);
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        repack<GT>(x.w[v]);
-        if (v * TH < x.vecs) {
-#pragma unroll
-            for (int q = 0; q < K; ++q) add_term(elem_of<GT>(x.w[v], q), b, c, s, u);
-        }
-        __builtin_amdgcn_sched_barrier(0);
+    for (int l = 0; l < LANES; ++l) {
+        move_base(base[l], M, c, s[l], u[l]);
+        group_put<OpSum>(s[l], red[0] + l * NW);
+        group_put<OpSum>(u[l], red[1] + l * NW);
     }
-    group_put<OpSum>(s, sh.red[2]);
-    group_put<OpSum>(u, more);
 
-    // as k_top
-    const int groups = min(x.vecs, a.top <= TH / kGroups ? TH : TH * kGroups);
+    // where the groups are not several times as many as are wanted, every logit of a short row
+    // is a candidate; fewer groups than wanted logits bound nothing
+    const int groups = min(vecs, a.top <= TH / G ? TH : TH * G);
     const bool all = 2 * a.top > groups && V <= kRoom, unbound = !all && groups < a.top;
     uint32_t least = 0;
     if (a.top == 0 || all || unbound)
         __syncthreads();
     else
         least = find_bound<TH>(sh, (uint32_t)a.top, M, m);
-    const float total = group_get<OpSum, NW>(sh.red[2]);
-    const RowScore r = row_score(M, total, group_get<OpSum, NW>(more));
+    const float total = group_get<OpSum, 16>(red[0]);
+    const RowScore r = row_score(M, total, group_get<OpSum, 16>(red[1]));
     if (tid == 0) put_row(a, row, r, token);
     if (a.top == 0) return;
     bool counted = total != total || unbound;
     if (!counted) {                                      // collect
         const float bound = key_value(least);
-        if (x.has_last(V) && (all || x.last >= bound)) offer<TH>(sh, x.last, x.last_column());
+        if (has_last && (all || last >= bound)) offer<TH>(sh, last, whole + tid);
+        auto take = [&](int i) __attribute__((always_inline)) {
+            const u32x4 w = *reinterpret_cast<const u32x4_a2 *>(z + (int64_t)i * K);
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            repack<GT>(x.w[v]);
-            if (x.at(v) < x.vecs && (all || max_of<GT>(x.w[v]) >= bound)) {
-#pragma unroll
-                for (int q = 0; q < K; ++q) {
-                    const float e = elem_of<GT>(x.w[v], q);
-                    if (all || e >= bound) offer<TH>(sh, e, x.at(v) * K + q);
-                }
+            for (int q = 0; q < K; ++q) {
+                const float e = elem_of<GT>(w, q);
+                if (all || e >= bound) offer<TH>(sh, e, (int64_t)i * K + q);
             }
-            __builtin_amdgcn_sched_barrier(0);
-        }
+        };
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+            if (all || m.of[g] >= bound)
+                for (int i = tid + g * TH; i < vecs; i += G * TH) take(i);
         __syncthreads();
         counted = sh.sel[3] > kRoom;
     }
@@ -162,88 +261,18 @@ __global__ __launch_bounds__(TH, TH == 768 ? 6 : 4) void k_score(zo_score a)
         sort_out<TH>(sh, (int)sh.sel[3], a.top, PutScore{a, row, r});
 }
 
-// Rows that do not fit registers: the largest logits of the groups first, then, in a second
-// read, the sums and the candidates.
-template <int GT>
-__global__ __launch_bounds__(1024) void k_score_long(zo_score a)
-{
-    constexpr int TH = 1024, NW = TH / 64, K = Elem<GT>::kVec;
-    __shared__ TopShared<TH> sh;
-    __shared__ float more[NW];
-    const int tid = threadIdx.x;
-    const int64_t row = blockIdx.x, V = a.vocab;
-    const auto *z = static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ldz;
-    const Token token = read_token<GT>(a, row, z);
-    const float c = log2_factor(a.tau);
-    for (int i = tid; i < 256; i += TH) sh.hist[i] = 0;
-    if (tid == 0) sh.sel[3] = 0;
-    GroupMaxima m = {-INFINITY, {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, 0};
-    for (int64_t i0 = (int64_t)tid * K; i0 < V; i0 += kGroups * TH * K) {
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-            const int64_t i = i0 + g * TH * K;
-            m.of[g] = fmaxf(m.of[g],
-                            max_of<GT>(load16<GT>(z + i, V - i, kNegInf<GT> & kElemMask<GT>)));
-            if (i < V) m.there |= 1u << g;
-        }
-    }
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) m.all = fmaxf(m.all, m.of[g]);
-    group_put<OpMax>(m.all, sh.red[0]);
-    __syncthreads();
-    const float M = group_get<OpMax, NW>(sh.red[0]), b = M == -INFINITY ? 0.0f : M;
-    const bool wanted = a.top > 0;
-    const float bound = wanted ? key_value(find_bound<TH>(sh, (uint32_t)a.top, M, m)) : 0.0f;
-    float s = 0.0f, u = 0.0f;
-    for (int64_t i = (int64_t)tid * K; i < V; i += TH * K) {
-        const u32x4 w = load16<GT>(z + i, V - i, kNegInf<GT> & kElemMask<GT>);
-#pragma unroll
-        for (int q = 0; q < K; ++q) add_term(elem_of<GT>(w, q), b, c, s, u);
-        if (wanted && max_of<GT>(w) >= bound) {
-#pragma unroll
-            for (int q = 0; q < K; ++q) {
-                const float e = elem_of<GT>(w, q);
-                if (e >= bound && i + q < V) offer<TH>(sh, e, i + q);
-            }
-        }
-    }
-    group_put<OpSum>(s, sh.red[2]);
-    group_put<OpSum>(u, more);
-    __syncthreads();
-    const float total = group_get<OpSum, NW>(sh.red[2]);
-    const RowScore r = row_score(M, total, group_get<OpSum, NW>(more));
-    if (tid == 0) put_row(a, row, r, token);
-    if (!wanted) return;
-    const uint32_t n = sh.sel[3];
-    if (total != total || n > kRoom)
-        select_row<GT, TH>(z, V, a.top, sh, PutScore{a, row, r});
-    else
-        sort_out<TH>(sh, (int)n, a.top, PutScore{a, row, r});
-}
-
+// 1024 vectors at most are one for each lane.  Of long rows, four workgroups of 512 threads a
+// CU, or, where a CU has no more than two rows, of 1024: 4096 x 50304 bfloat16, 20 wanted, 106 us
+// against 122; 3 x 50257 binary32, 5 wanted, 12.8 against 10.6.  More wanted logits need the
+// groups of 1024 threads.
 static hipError_t launch_rows(const zo_score &a, int gt, hipStream_t st)
 {
     return with_elem_type(gt, [&](auto g) {
         constexpr int GT = decltype(g)::value;
         const int64_t vecs = a.vocab / Elem<GT>::kVec;
-        auto go = [&](auto th, auto nv) {
-            constexpr int TH = decltype(th)::value, NV = decltype(nv)::value;
-            return start(k_score<GT, TH, NV>, a.rows, TH, 0, st, a);
-        };
-        using std::integral_constant;
-        if (vecs > 1024 * 16) return start(k_score_long<GT>, a.rows, 1024, 0, st, a);
-        // as for the top logits
-        if (a.top <= 256 && vecs <= 256 * 4)
-            return go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
-        if (a.top <= 256 && vecs <= 256 * 8)
-            return go(integral_constant<int, 256>{}, integral_constant<int, 8>{});
-        if (a.top <= 512 && vecs <= 512 * 8)
-            return go(integral_constant<int, 512>{}, integral_constant<int, 8>{});
-        if (a.top <= 768 && vecs <= 768 * 9)
-            return go(integral_constant<int, 768>{}, integral_constant<int, 9>{});
-        if (a.top <= 768 && vecs <= 768 * 11)
-            return go(integral_constant<int, 768>{}, integral_constant<int, 11>{});
-        return go(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
+        if (a.top <= 256 && vecs <= 1024) return start(k_score<GT, 256>, a.rows, 256, 0, st, a);
+        if (a.top <= 256 && a.rows > 512) return start(k_score<GT, 512>, a.rows, 512, 0, st, a);
+        return start(k_score<GT, 1024>, a.rows, 1024, 0, st, a);
     });
 }
 

@@ -154,6 +154,47 @@ def test_score_outputs(torch):
     assert torch.equal(v, values) and torch.equal(c, columns)
 
 
+@pytest.mark.parametrize("dtype,vocab", [("bfloat16", 8000), ("float32", 20001),
+                                         ("bfloat16", 50257)])
+def test_score_same_bits_in_any_batch(torch, dtype, vocab):
+    """A row's sums do not depend on the other rows or on how many alternatives are wanted:
+    the forms for few rows, many rows and many alternatives."""
+    z = _logits(torch, 700, vocab, dtype, seed=8, pad=1)
+    tokens = _tokens(torch, z, seed=8)
+    many = _score(torch, z, tokens, 20)
+    for rows, top in ((3, 20), (700, 0), (3, 0), (5, 300), (700, 300)):
+        got = _score(torch, z[:rows], tokens[:rows], top)
+        assert torch.equal(got[0], many[0][:rows]) and torch.equal(got[1], many[1][:rows])
+        if top:
+            assert torch.equal(got[2][:, :20], many[2][:rows])
+            assert torch.equal(got[3][:, :20], many[3][:rows])
+
+
+@pytest.mark.parametrize("tau", [2.0 ** -126, 2.0 ** -20, 2.0 ** 20, 2.0 ** 125, 3e38])
+def test_score_extreme_tau(torch, tau):
+    """Temperatures near binary32's ends: one logit has everything, or all are alike.  A
+    distance over tau that passes binary32 is -infinity."""
+    z = _logits(torch, 4, 3000, "float32", seed=2)
+    z[1, 5] = -torch.inf
+    z[2, :2500] = -torch.inf
+    tokens = torch.tensor([7, 5, 2600, 9], dtype=torch.int32, device="cuda")
+    tau = float(torch.tensor(tau))
+    _check(torch, z, tokens, 5, tau, _score(torch, z, tokens, 5, tau))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_score_growing_rows(torch, dtype):
+    """Each vector far above the ones before it, and the first ones masked: the sums are moved
+    on the way."""
+    z = _logits(torch, 3, 9001, dtype, seed=5)
+    step = torch.arange(9001, device="cuda") // 500
+    z[0] += (step * 100).to(z.dtype)
+    z[1, :8500] = -torch.inf
+    z[2, 4000:] += 3000
+    tokens = torch.tensor([9000, 8700, 4100], dtype=torch.int32, device="cuda")
+    _check(torch, z, tokens, 30, 1.0, _score(torch, z, tokens, 30))
+
+
 def _check_grad(torch, z, tokens, tau, dlogp, dentropy, dz, rows=None):
     import i8_ref as ref
     stats = ref.score(z.double(), None, tau)[1]
