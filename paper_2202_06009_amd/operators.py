@@ -98,9 +98,10 @@ class I8:
         if codes.dtype is not torch.int8 or scales.dtype is not torch.float32:
             raise ValueError(f"codes, scales: expected int8 and float32, got {codes.dtype} and "
                              f"{scales.dtype}")
-        for t, k, what in ((codes, n, "codes"), (scales, rows, "scales")):
-            if t.numel() < k or not t.is_contiguous():
-                raise ValueError(f"{what}: needs {k} contiguous elements, has {t.numel()}")
+        if codes.numel() < n or not codes.is_contiguous():
+            raise ValueError(f"codes: needs {n} contiguous elements, has {codes.numel()}")
+        if scales.numel() < rows or not scales.is_contiguous():
+            raise ValueError(f"scales: needs {rows} contiguous elements, has {scales.numel()}")
         dev = codes.get_device()
         if dev < 0 or scales.get_device() != dev:
             raise ValueError("codes, scales: expected tensors on one GPU")
