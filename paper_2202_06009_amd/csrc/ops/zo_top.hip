@@ -23,12 +23,16 @@ namespace zo {
 
 // Writes a row's result.
 struct PutLogit {
-    const TopArgs &a;
-    int64_t row;
+    float *values;
+    int32_t *columns;
+    __device__ __forceinline__ PutLogit(const TopArgs &a, int64_t row)
+        : values(a.values + row * a.top), columns(a.columns + row * a.top)
+    {
+    }
     __device__ __forceinline__ void operator()(int rank, uint64_t key) const
     {
-        a.values[row * a.top + rank] = key_value((uint32_t)(key >> 32));
-        a.columns[row * a.top + rank] = (int32_t)~(uint32_t)key;
+        values[rank] = key_value((uint32_t)(key >> 32));
+        columns[rank] = (int32_t)~(uint32_t)key;
     }
 };
 
@@ -126,7 +130,7 @@ __global__ __launch_bounds__(1024) void k_top_long(TopArgs a)
     const float total = group_get<OpSum, NW>(s.red[2]);
     if (total != total) {                                // NaN or an infinity is about
         if (a.lse) lse_row<GT, TH>(a, row, s);
-        select_row<GT, TH>(z, V, a.top, s, PutLogit{a, row});
+        select_row<GT, TH>(z, V, a.top, s, PutLogit(a, row));
         return;
     }
     if (a.lse && tid == 0) a.lse[row] = lse_of(M, total, a.tau, false);
@@ -144,9 +148,9 @@ __global__ __launch_bounds__(1024) void k_top_long(TopArgs a)
     __syncthreads();
     const uint32_t n = s.sel[3];
     if (n > kRoom)
-        select_row<GT, TH>(z, V, a.top, s, PutLogit{a, row});
+        select_row<GT, TH>(z, V, a.top, s, PutLogit(a, row));
     else
-        sort_out<TH>(s, (int)n, a.top, PutLogit{a, row});
+        sort_out<TH>(s, (int)n, a.top, PutLogit(a, row));
 }
 
 template <int GT, int TH, int NV>
@@ -226,9 +230,9 @@ __global__ __launch_bounds__(TH, TH == 768 ? 6 : 4) void k_top(TopArgs a)
         counted = s.sel[3] > kRoom;
     }
     if (counted)
-        select_row<GT, TH>(z, V, a.top, s, PutLogit{a, row});
+        select_row<GT, TH>(z, V, a.top, s, PutLogit(a, row));
     else
-        sort_out<TH>(s, (int)s.sel[3], a.top, PutLogit{a, row});
+        sort_out<TH>(s, (int)s.sel[3], a.top, PutLogit(a, row));
     if (a.lse && !plain) lse_row<GT, TH>(a, row, s);     // the row's registers are free
 }
 
