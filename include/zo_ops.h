@@ -26,6 +26,7 @@
  *   - Sums, softmax statistics and products accumulate in binary32; a result
  *     is rounded once, to nearest even, to the type of its buffer.
  *   - Results depend on the inputs alone: no atomics decide an order of sums.
+ *   - Calls that may run at once need workspaces of their own.
  */
 #ifndef ZO_OPS_H
 #define ZO_OPS_H

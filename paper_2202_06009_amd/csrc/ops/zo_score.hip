@@ -5,7 +5,6 @@
 //   S = sum e, U = sum e t; log p = (z - m) / tau - ln S, entropy = ln S - ln 2 U / S.
 // A logit of -infinity adds nothing to either sum: where the product of 0 and -infinity has
 // made U a NaN, the vector is taken again with t clamped to kLeast.
-//
 #include "zo_top_device.h"
 
 namespace zo {
