@@ -349,9 +349,9 @@ typedef struct zo_score {
  * zo_token_logprobs -- per row, with d = (z - m) / tau:
  *   log p = d - log S, entropy = log S - sum of exp(d) d / S,
  * in one read of the logits.  A row's results are the same bits in any batch and
- * whatever else is wanted.  A logit of -infinity has log p = -infinity and adds 0 to the entropy.  A row of only -infinity has the
- * statistics -infinity, -infinity, 0 and log probabilities of -infinity; in one with a
- * NaN or +infinity all of them are NaN.
+ * whatever else is wanted.  A logit of -infinity has log p = -infinity and adds 0 to
+ * the entropy.  A row of only -infinity has the statistics -infinity, -infinity, 0 and
+ * log probabilities of -infinity; in one with a NaN or +infinity all of them are NaN.
  */
 int zo_token_logprobs(const zo_score *args, hipStream_t stream);
 
