@@ -130,7 +130,8 @@ __device__ __forceinline__ void add_vector(const u32x4 &w, float b, float c, flo
     }
 }
 
-// The sums about a larger logit than they were; from -infinity they are 0, or a NaN.
+// The sums about a larger logit than they were: u and s d are both below 0, so nothing cancels.
+// From -infinity they are 0, or a NaN.
 __device__ __forceinline__ void move_base(float from, float to, float c, float &s, float &u)
 {
     if (from == -INFINITY) return;
@@ -141,9 +142,12 @@ __device__ __forceinline__ void move_base(float from, float to, float c, float &
 
 // A row by TH threads, in one read.  The sums are those of 1024 lanes, of which a thread is
 // one, two or four: lane l takes the vectors l, l + 1024, ... of the row and sums about the
-// largest logit of its first, moved only when one is 2^64 times as likely; the sums of waves of
+// largest logit of the row's first 1024 vectors, or a larger one of its own; the sums of waves of
 // 64 lanes are joined in order.  So a row's results
-// are the same bits however many rows there are and whatever else is wanted.
+// are the same bits however many rows there are and whatever else is wanted.  No logit is larger
+// than what its lane sums about: a term is at most 1, the row's largest exactly, so S >= 1 and no
+// log probability is above 0.  About each lane's own first vector a base would move with most of
+// a wave's vectors; beyond the first 1024 hardly any holds a larger one.
 //
 // Every N-th of a lane's vectors belongs to the same group, four groups a thread.  The groups' maxima bound the k-th
 // largest logit from below, and only those that reach the bound, few more than are wanted, are
@@ -167,7 +171,6 @@ __global__ __launch_bounds__(TH, 8) void k_score(zo_score a)
     const float c = log2_factor(a.tau);
     GroupMaxima m = {-INFINITY, {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, 0};
     float base[LANES], s[LANES] = {}, u[LANES] = {};
-    const float slack = fminf(64.0f / c, 0x1.fffffep127f);
 #pragma unroll
     for (int l = 0; l < LANES; ++l) base[l] = -INFINITY;
     for (int j = 0; j < vecs; j += 1024 * N) {
@@ -181,6 +184,16 @@ __global__ __launch_bounds__(TH, 8) void k_score(zo_score a)
                 const int i = min(j + n * 1024 + l * TH + tid, vecs - 1);
                 w[n][l] = *reinterpret_cast<const u32x4_a2 *>(z + (int64_t)i * K);
             }
+        if (j == 0) {                                    // w[0]: the first 1024 vectors
+            float top = largest_of<GT>(w[0][0]);
+#pragma unroll
+            for (int l = 1; l < LANES; ++l) top = fmaxf(top, largest_of<GT>(w[0][l]));
+            group_put<OpMax>(top, sh.red[2]);
+            __syncthreads();
+            top = group_get<OpMax, NW>(sh.red[2]);
+#pragma unroll
+            for (int l = 0; l < LANES; ++l) base[l] = top;
+        }
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -190,7 +203,7 @@ __global__ __launch_bounds__(TH, 8) void k_score(zo_score a)
                     const float top = largest_of<GT>(w[n][l]);
                     m.of[g] = fmaxf(m.of[g], top);
                     m.there |= 1u << g;
-                    if (top > base[l] + slack) {
+                    if (top > base[l]) {
                         move_base(base[l], top, c, s[l], u[l]);
                         base[l] = top;
                     }
@@ -201,7 +214,7 @@ __global__ __launch_bounds__(TH, 8) void k_score(zo_score a)
     const bool has_last = whole + tid < V;
     const float last = has_last ? widen<GT>(z[whole + tid]) : -INFINITY;
     if (has_last) {
-        if (last > base[0] + slack) {
+        if (last > base[0]) {
             move_base(base[0], last, c, s[0], u[0]);
             base[0] = last;
         }
