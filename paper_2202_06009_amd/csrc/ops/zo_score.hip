@@ -3,6 +3,8 @@
 //
 // With m the row's largest logit, t = (z - m) log2(e) / tau and e = 2^t:
 //   S = sum e, U = sum e t; log p = (z - m) / tau - ln S, entropy = ln S - ln 2 U / S.
+// Where one logit has more than half of the probability, S - 1 is summed apart from its 1, and
+// ln S is log1p of that: log p of that token keeps its digits, and 1 - p in the gradient.
 // A logit of -infinity adds nothing to either sum: where the product of 0 and -infinity has
 // made U a NaN, the vector is taken again with t clamped to kLeast.
 #include "zo_top_device.h"
@@ -33,12 +35,12 @@ struct PutScore {
     }
 };
 
-// From the sums; s of NaN: a NaN or +infinity is among the logits.
-__device__ __forceinline__ RowScore row_score(float m, float s, float u)
+// From the sums, and s - 1 where s is below 2; s of NaN: a NaN or +infinity is among the logits.
+__device__ __forceinline__ RowScore row_score(float m, float s, float rest, float u)
 {
     if (s != s) return {NAN, NAN, NAN};
     if (m == -INFINITY) return {m, m, 0.0f};
-    const float log_s = logf(s);
+    const float log_s = s < 2.0f ? log1pf(rest) : logf(s);
     return {m, log_s, fmaxf(log_s - kLn2 * (u / s), 0.0f)};
 }
 
@@ -109,6 +111,12 @@ __device__ __forceinline__ void add_term(float z, float b, float c, float &s, fl
     const float t = (z - b) * c, e = exp2_hw(t);
     s += e;
     u = __builtin_fmaf(e, fmaxf(t, kLeast), u);
+}
+
+// The same of the row's largest logit m, less the 1 that it is itself.
+__device__ __forceinline__ void add_other(float z, float m, float c, float &s, float &u)
+{
+    add_term(z == m ? -INFINITY : z, m, c, s, u);
 }
 
 // A vector's terms about b.
@@ -234,18 +242,49 @@ __global__ __launch_bounds__(TH, 8) void k_score(zo_score a)
         group_put<OpSum>(s[l], red[0] + l * NW);
         group_put<OpSum>(u[l], red[1] + l * NW);
     }
+    __syncthreads();
+    const float total = group_get<OpSum, 16>(red[0]);
+    float rest = 0.0f, mean = group_get<OpSum, 16>(red[1]);
+    // S below 2: one logit alone is the largest, as another would add 1, and S has lost the last
+    // digits of the others to its 1.  The wave of the lane that has it takes that lane's logits
+    // again, one a thread, without it (4096 x 50304 bfloat16 with only such rows 86 us, the lane by
+    // itself 93, S as it is 79)
+    if (total < 2.0f && M > -INFINITY) {                 // the same for all
+        __syncthreads();
+#pragma unroll
+        for (int l = 0; l < LANES; ++l) {
+            float top = l == 0 ? last : -INFINITY;
+#pragma unroll
+            for (int n = 0; n < N; ++n) top = fmaxf(top, m.of[n * LANES + l]);
+            if (const uint64_t mine = __ballot(top == M)) {
+                const int at = __ffsll((unsigned long long)mine) - 1, id = tid & 63;
+                const int first = l * TH + tid - id + at;        // the lane
+                float so = 0.0f, uo = 0.0f;
+                for (int k = id; first + k / K * 1024 < vecs; k += 64)
+                    add_other(widen<GT>(z[(int64_t)(first + k / K * 1024) * K + k % K]), M, c, so, uo);
+                if (l == 0 && id == at) add_other(last, M, c, so, uo);
+                so = wave_reduce<OpSum>(so);
+                uo = wave_reduce<OpSum>(uo);
+                if (id == at) {
+                    s[l] = so;
+                    u[l] = uo;
+                }
+            }
+            group_put<OpSum>(s[l], red[0] + l * NW);
+            group_put<OpSum>(u[l], red[1] + l * NW);
+        }
+        __syncthreads();
+        rest = group_get<OpSum, 16>(red[0]);
+        mean = group_get<OpSum, 16>(red[1]);
+    }
 
     // where the groups are not several times as many as are wanted, every logit of a short row
     // is a candidate; fewer groups than wanted logits bound nothing
     const int groups = min(vecs, a.top <= TH / G ? TH : TH * G);
     const bool all = 2 * a.top > groups && V <= kRoom, unbound = !all && groups < a.top;
     uint32_t least = 0;
-    if (a.top == 0 || all || unbound)
-        __syncthreads();
-    else
-        least = find_bound<TH>(sh, (uint32_t)a.top, M, m);
-    const float total = group_get<OpSum, 16>(red[0]);
-    const RowScore r = row_score(M, total, group_get<OpSum, 16>(red[1]));
+    if (a.top > 0 && !all && !unbound) least = find_bound<TH>(sh, (uint32_t)a.top, M, m);
+    const RowScore r = row_score(M, total, rest, mean);
     if (tid == 0) put_row(a, row, r, token);
     if (a.top == 0) return;
     bool counted = total != total || unbound;

@@ -38,7 +38,8 @@ def off(z, tau, vec, apart, count=None):
     2 U, product, and what is of second order), so a term by 5 ln 2 U T, below 3.5 U T, and by a
     step, 2 U, of the exponential; each move by a step and a product more, 3 U; sums of positive
     terms by U for each of n terms and 6 + 16 joins; terms below 2^-126 may be 0.  `apart`: whether
-    the 1 of the largest logit is left out where S < 2, else it is a term as the others.  `count`:
+    the 1 of the largest logit is left out where S < 2 (its lane's other terms are then added by 64
+    threads and 6 joins, in the place of its moves), else it is a term as the others.  `count`:
     the roundings of a sum where they are fewer than that."""
     vocab = z.shape[1]
     if count is None:

@@ -112,3 +112,77 @@ def test_entropy_of_few_logits(torch, dtype):
             float(((stats[:, 2] - want[:, 2]).abs() / h_off).max())))
         assert bool(((stats[:, 1] - want[:, 1]).abs() <= log_off).all())
         assert bool(((stats[:, 2] - want[:, 2]).abs() <= h_off).all())
+
+
+@pytest.mark.parametrize("dtype,vocab", CASES + [("float32", 9), ("bfloat16", 1003), ("float32", 140001)])
+def test_confident_rows_keep_their_digits(torch, dtype, vocab):
+    """log S = log1p(S - 1) where the largest logit has more than half of the row's probability,
+    S - 1 summed apart from its 1: log probabilities and entropies down to 1e-18 are right in
+    relation to themselves."""
+    import score_ref as ref
+    for tau in (1.0, 0.7):
+        z, at = _peaked(torch, vocab, dtype, [2 + 0.7 * i for i in range(64)], seed=vocab + 1)
+        at = z.argmax(1).int()
+        logp, stats, _, _ = _score(torch, z, at, 3, tau)
+        t = float(torch.tensor(tau))
+        want, want_stats = ref.score(z.double(), at, t)
+        log_off, h_off = ref.off(z.double(), t, _vec(z), apart=True)
+        log_err, h_err = (stats[:, 1:].double() - want_stats[:, 1:]).abs().unbind(1)
+        print("log S %.2f, entropy %.2f of the bound, log S from %.1e, bounds up to %.1e of it" % (
+            float((log_err / log_off).max()), float((h_err / h_off).max()),
+            float(want_stats[:, 1].min()), float((log_off / want_stats[:, 1]).max())))
+        assert bool((log_err <= log_off).all()) and bool((h_err <= h_off).all())
+        # the largest logit's log probability is the same number but for its sign
+        assert torch.equal(logp, -stats[:, 1])
+
+
+def test_equal_largest_logits(torch):
+    """Two or more of them, in one vector, one lane, two lanes, among the last columns: each counts."""
+    import score_ref as ref
+    vocab = 20003
+    for dtype in DTYPES:
+        z = torch.randn((8, vocab), generator=torch.Generator().manual_seed(1)).to(getattr(torch, dtype))
+        turn = 1024 * _vec(z)
+        for i, cols in enumerate(([5], [5, 6], [5, 5 + turn], [5, 900], [vocab - 1], [vocab - 1, 7],
+                                  [vocab - 1, vocab - 2], list(range(100)))):
+            z[i, cols] = 30.0
+        z = z.cuda()
+        at = torch.tensor([5, 6, 5, 900, vocab - 1, 7, vocab - 2, 99], dtype=torch.int32, device="cuda")
+        _, stats, values, columns = _score(torch, z, at, 2, 1.0)
+        want = ref.score(z.double(), at, 1.0)[1]
+        log_off, h_off = ref.off(z.double(), 1.0, _vec(z), apart=True)
+        assert bool(((stats[:, 1] - want[:, 1]).abs() <= log_off).all())
+        assert bool(((stats[:, 2] - want[:, 2]).abs() <= h_off).all())
+
+
+@pytest.mark.parametrize("dtype,vocab", [("float32", 9), ("float32", 8195), ("bfloat16", 50304)])
+def test_gradient_of_confident_tokens(torch, dtype, vocab):
+    """dz of the token, dlogp (1 - p) - dentropy p (log p + entropy), from the statistics of the
+    forward pass, in relation to itself.  1 - p is off by as much as log p and by expm1's two steps;
+    p (log p + entropy) by both statistics; each of five operations more by U, 8 U with p's
+    exponential."""
+    import i8_ref
+    import paper_2202_06009_amd as zo
+    import score_ref as ref
+    z, _ = _peaked(torch, vocab, dtype, [3 + 0.6 * i for i in range(64)], seed=5)
+    at = z.argmax(1).int()
+    _, stats, _, _ = _score(torch, z, at, 3, 1.0)
+    want_logp, want = ref.score(z.double(), at, 1.0)
+    log_off, h_off = ref.off(z.double(), 1.0, _vec(z), apart=True)
+    one = torch.ones(64, device="cuda")
+    for dlogp, dentropy in ((one, None), (None, one), (one, -0.25 * one)):
+        dz = torch.empty_like(z)
+        zo.zo_token_logprobs_grad(z, stats, dz, tokens=at, dlogp=dlogp, dentropy=dentropy)
+        got = dz.gather(1, at.long()[:, None])[:, 0].double()
+        a = 0.0 if dlogp is None else 1.0
+        b = 0.0 if dentropy is None else float(dentropy[0])
+        p, h = want_logp.exp(), want[:, 2]
+        first, second = -a * torch.expm1(want_logp), -b * p * (want_logp + h)
+        off = a * (log_off + 5 * ref.U * want_logp.abs())
+        off += abs(b) * (log_off + h_off + 8 * ref.U * (want_logp.abs() + h))
+        off += 8 * ref.U * (first.abs() + second.abs())
+        dt = z.dtype
+        off = off + i8_ref.HALF[dt] * ((first + second).abs() + off) + i8_ref.TINY[dt]
+        err = (got - first - second).abs()
+        print("%.2f of the bound" % float((err / off).max()))
+        assert bool((err <= off).all())
