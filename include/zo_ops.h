@@ -350,7 +350,8 @@ typedef struct zo_score {
  *   log p = d - log S, entropy = log S - sum of exp(d) d / S,
  * in one read of the logits.  Where S < 2, S - 1 is formed apart from its 1: log S, the
  * largest log probability and the entropy are then right in relation to themselves, down
- * to terms of 2^-126.  log S and the entropy are not below 0, log p not above.  A row's results are the same bits in any batch and
+ * to terms of 2^-126.  log S and the entropy are not below 0, log p not above.  A d that
+ * passes binary32 is -infinity; a difference z - m may pass it.  A row's results are the same bits in any batch and
  * whatever else is wanted.  A logit of -infinity has log p = -infinity and adds 0 to
  * the entropy.  A row of only -infinity has the statistics -infinity, -infinity, 0 and
  * log probabilities of -infinity; in one with a NaN or +infinity all of them are NaN.

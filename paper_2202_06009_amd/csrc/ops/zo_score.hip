@@ -13,6 +13,24 @@ namespace zo {
 
 constexpr float kLeast = -256.0f;
 
+// Distances over tau, from k z - k m: with a k of 1/4 for a tau of 1 or more the difference of the
+// largest numbers stays within binary32, and the factor of the largest tau within its normal
+// numbers.  Below 1 a distance that passes binary32 does so over tau too.
+struct Slope {
+    float k, c;                  // c = log2(e) / (k tau)
+
+    __device__ __forceinline__ explicit Slope(float tau)
+        : k(tau < 1.0f ? 1.0f : 0.25f), c(kLog2e / (k * tau))
+    {
+    }
+    // k (z - m), and t of it.
+    __device__ __forceinline__ float apart(float z, float m) const
+    {
+        return __builtin_fmaf(z, k, -(k * m));
+    }
+    __device__ __forceinline__ float octaves(float z, float m) const { return apart(z, m) * c; }
+};
+
 // A row's results.
 struct RowScore {
     float m, log_s, entropy;
@@ -20,8 +38,9 @@ struct RowScore {
 
 __device__ __forceinline__ float log_prob(float z, const RowScore &r, float tau)
 {
+    const Slope by(tau);
     if (r.log_s != r.log_s) return NAN;
-    return z == -INFINITY ? -INFINITY : (z - r.m) / tau - r.log_s;
+    return z == -INFINITY ? -INFINITY : by.apart(z, r.m) / (by.k * tau) - r.log_s;
 }
 
 struct PutScore {
@@ -106,27 +125,29 @@ __device__ __forceinline__ void put_row(const zo_score &a, int64_t row, const Ro
     }
 }
 
-__device__ __forceinline__ void add_term(float z, float b, float c, float &s, float &u)
+__device__ __forceinline__ void add_term(float z, float b, const Slope &by, float &s, float &u)
 {
-    const float t = (z - b) * c, e = exp2_hw(t);
+    const float t = by.octaves(z, b), e = exp2_hw(t);
     s += e;
     u = __builtin_fmaf(e, fmaxf(t, kLeast), u);
 }
 
 // The same of the row's largest logit m, less the 1 that it is itself.
-__device__ __forceinline__ void add_other(float z, float m, float c, float &s, float &u)
+__device__ __forceinline__ void add_other(float z, float m, const Slope &by, float &s,
+                                          float &u)
 {
-    add_term(z == m ? -INFINITY : z, m, c, s, u);
+    add_term(z == m ? -INFINITY : z, m, by, s, u);
 }
 
 // A vector's terms about b.
 template <int GT>
-__device__ __forceinline__ void add_vector(const u32x4 &w, float b, float c, float &s, float &u)
+__device__ __forceinline__ void add_vector(const u32x4 &w, float b, const Slope &by, float &s,
+                                           float &u)
 {
     const float s0 = s, u0 = u;
 #pragma unroll
     for (int q = 0; q < Elem<GT>::kVec; ++q) {
-        const float t = (elem_of<GT>(w, q) - b) * c, e = exp2_hw(t);
+        const float t = by.octaves(elem_of<GT>(w, q), b), e = exp2_hw(t);
         s += e;
         u = __builtin_fmaf(e, t, u);
     }
@@ -134,16 +155,17 @@ __device__ __forceinline__ void add_vector(const u32x4 &w, float b, float c, flo
         s = s0;
         u = u0;
 #pragma unroll
-        for (int q = 0; q < Elem<GT>::kVec; ++q) add_term(elem_of<GT>(w, q), b, c, s, u);
+        for (int q = 0; q < Elem<GT>::kVec; ++q) add_term(elem_of<GT>(w, q), b, by, s, u);
     }
 }
 
 // The sums about a larger logit than they were: u and s d are both below 0, so nothing cancels.
 // From -infinity they are 0, or a NaN.
-__device__ __forceinline__ void move_base(float from, float to, float c, float &s, float &u)
+__device__ __forceinline__ void move_base(float from, float to, const Slope &by, float &s,
+                                          float &u)
 {
     if (from == -INFINITY) return;
-    const float d = fmaxf((from - to) * c, kLeast), f = exp2_hw(d);
+    const float d = fmaxf(by.octaves(from, to), kLeast), f = exp2_hw(d);
     u = f * __builtin_fmaf(s, d, u);
     s *= f;
 }
@@ -176,7 +198,7 @@ __global__ __launch_bounds__(TH, 8) void k_score(zo_score a)
     const int64_t row = blockIdx.x, V = a.vocab, whole = (int64_t)vecs * K;
     const auto *z = static_cast<const typename Elem<GT>::T *>(a.z) + row * a.ldz;
     const Token token = read_token<GT>(a, row, z);
-    const float c = log2_factor(a.tau);
+    const Slope by(a.tau);
     GroupMaxima m = {-INFINITY, {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, 0};
     float base[LANES], s[LANES] = {}, u[LANES] = {};
 #pragma unroll
@@ -212,10 +234,10 @@ __global__ __launch_bounds__(TH, 8) void k_score(zo_score a)
                     m.of[g] = fmaxf(m.of[g], top);
                     m.there |= 1u << g;
                     if (top > base[l]) {
-                        move_base(base[l], top, c, s[l], u[l]);
+                        move_base(base[l], top, by, s[l], u[l]);
                         base[l] = top;
                     }
-                    add_vector<GT>(w[n][l], base[l] == -INFINITY ? 0.0f : base[l], c, s[l], u[l]);
+                    add_vector<GT>(w[n][l], base[l] == -INFINITY ? 0.0f : base[l], by, s[l], u[l]);
                 }
     }
     // one each of the V % K logits that are left
@@ -223,10 +245,10 @@ __global__ __launch_bounds__(TH, 8) void k_score(zo_score a)
     const float last = has_last ? widen<GT>(z[whole + tid]) : -INFINITY;
     if (has_last) {
         if (last > base[0]) {
-            move_base(base[0], last, c, s[0], u[0]);
+            move_base(base[0], last, by, s[0], u[0]);
             base[0] = last;
         }
-        add_term(last, base[0] == -INFINITY ? 0.0f : base[0], c, s[0], u[0]);
+        add_term(last, base[0] == -INFINITY ? 0.0f : base[0], by, s[0], u[0]);
     }
     for (int i = tid; i < 256; i += TH) sh.hist[i] = 0;
     if (tid == 0) sh.sel[3] = 0;
@@ -238,7 +260,7 @@ __global__ __launch_bounds__(TH, 8) void k_score(zo_score a)
     const float M = group_get<OpMax, NW>(sh.red[0]);
 #pragma unroll
     for (int l = 0; l < LANES; ++l) {
-        move_base(base[l], M, c, s[l], u[l]);
+        move_base(base[l], M, by, s[l], u[l]);
         group_put<OpSum>(s[l], red[0] + l * NW);
         group_put<OpSum>(u[l], red[1] + l * NW);
     }
@@ -261,8 +283,9 @@ __global__ __launch_bounds__(TH, 8) void k_score(zo_score a)
                 const int first = l * TH + tid - id + at;        // the lane
                 float so = 0.0f, uo = 0.0f;
                 for (int k = id; first + k / K * 1024 < vecs; k += 64)
-                    add_other(widen<GT>(z[(int64_t)(first + k / K * 1024) * K + k % K]), M, c, so, uo);
-                if (l == 0 && id == at) add_other(last, M, c, so, uo);
+                    add_other(widen<GT>(z[(int64_t)(first + k / K * 1024) * K + k % K]), M, by, so,
+                              uo);
+                if (l == 0 && id == at) add_other(last, M, by, so, uo);
                 so = wave_reduce<OpSum>(so);
                 uo = wave_reduce<OpSum>(uo);
                 if (id == at) {
@@ -354,7 +377,7 @@ hipError_t launch_score(const zo_score &a, hipStream_t st)
 constexpr int kGradVecs = 4;
 
 // With t as above less log2 S, p = 2^t and log p = ln 2 t:
-//   dz = p (k0 + k1 t) / tau, k0 = -(dlogp + dentropy entropy), k1 = -ln 2 dentropy,
+//   dz = p (k0 + k1 t) / (k tau), k0 = -k (dlogp + dentropy entropy), k1 = -k ln 2 dentropy,
 // and at the token's column dlogp (1 - p) by expm1: 1 - p keeps its digits.
 // Workgroup (row, run of 256 kGradVecs vectors).
 template <int GT>
@@ -383,8 +406,9 @@ __global__ __launch_bounds__(256) void k_score_grad(zo_score_back a, uint32_t ru
         }
         return;
     }
-    const float c = log2_factor(a.tau), l2 = log_s * kLog2e;
-    const float k0 = -(dlogp + dh * h), k1 = -kLn2 * dh, scale = 1.0f / a.tau;
+    const Slope by(a.tau);
+    const float l2 = log_s * kLog2e, scale = 1.0f / (by.k * a.tau);
+    const float ga = by.k * dlogp, gh = by.k * dh, k0 = -(ga + gh * h), k1 = -kLn2 * gh;
     u32x4 w[kGradVecs];
 #pragma unroll
     for (int v = 0; v < kGradVecs; ++v) {
@@ -398,7 +422,8 @@ __global__ __launch_bounds__(256) void k_score_grad(zo_score_back a, uint32_t ru
         float e[K];
 #pragma unroll
         for (int q = 0; q < K; ++q) {
-            const float t = fmaxf(__builtin_fmaf(elem_of<GT>(w[v], q) - m, c, -l2), kLeast);
+            const float d = by.apart(elem_of<GT>(w[v], q), m);
+            const float t = fmaxf(__builtin_fmaf(d, by.c, -l2), kLeast);
             e[q] = exp2_hw(t) * __builtin_fmaf(k1, t, k0) * scale;
         }
         if (token >= i && token < i + K) {
@@ -406,9 +431,9 @@ __global__ __launch_bounds__(256) void k_score_grad(zo_score_back a, uint32_t ru
             for (int q = 0; q < K; ++q)
                 if (token == i + q) {
                     const float x = elem_of<GT>(w[v], q);
-                    const float lp = x == -INFINITY ? x : (x - m) / a.tau - log_s;
+                    const float lp = log_prob(x, RowScore{m, log_s, h}, a.tau);
                     const float t = fmaxf(lp * kLog2e, kLeast);
-                    e[q] = (-dlogp * expm1f(lp) - dh * exp2_hw(t) * (t * kLn2 + h)) * scale;
+                    e[q] = (-ga * expm1f(lp) - gh * exp2_hw(t) * (t * kLn2 + h)) * scale;
                 }
         }
         store16<GT>(dz + i, pack16<GT>(e), V - i);
