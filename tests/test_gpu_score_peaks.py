@@ -186,3 +186,54 @@ def test_gradient_of_confident_tokens(torch, dtype, vocab):
         err = (got - first - second).abs()
         print("%.2f of the bound" % float((err / off).max()))
         assert bool((err <= off).all())
+
+
+@pytest.mark.parametrize("dtype,vocab", [("bfloat16", 8000), ("bfloat16", 50304), ("float32", 20001)])
+def test_confident_rows_in_any_batch(torch, dtype, vocab):
+    """The same bits from the forms for short rows, few rows, many rows and many alternatives."""
+    z, _ = _peaked(torch, vocab, dtype, [5 + 0.05 * i for i in range(700)], seed=9)
+    at = z.argmax(1).int()
+    many = _score(torch, z, at, 20, 1.0)
+    for rows, top in ((3, 20), (500, 300), (700, 300), (700, 1)):
+        got = _score(torch, z[-rows:], at[-rows:], top, 1.0)
+        assert torch.equal(got[0], many[0][-rows:]) and torch.equal(got[1], many[1][-rows:])
+        n = min(top, 20)
+        assert torch.equal(got[2][:, :n], many[2][-rows:, :n])
+        assert torch.equal(got[3][:, :n], many[3][-rows:, :n])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab", [20003, 70001])
+def test_masked_confident_rows(torch, dtype, vocab):
+    """Masks of -infinity and of a low value before, around and behind the largest logit: the first
+    1024 vectors altogether, all but it, all but it and one more, every second; rows that grow
+    with every vector; a NaN beside them."""
+    import score_ref as ref
+    dt = getattr(torch, dtype)
+    z = torch.randn((10, vocab), generator=torch.Generator().manual_seed(2)) * 2
+    span = 1024 * (16 // torch.empty(0, dtype=dt).element_size())
+    low = float(torch.finfo(dt).min)
+    z[0, :span], z[0, span + 9] = -torch.inf, 25.0
+    z[1, :], z[1, -1] = -torch.inf, 3.0
+    z[2, :], z[2, -2], z[2, 17] = -torch.inf, 3.0, -20.0
+    z[3, ::2], z[3, span + 1] = -torch.inf, 30.0
+    z[4, :span], z[4, span + 9] = low, 25.0
+    z[5, :], z[5, 5], z[5, -1] = low, 2.0, 14.0
+    z[6] = torch.arange(vocab) // (span // 8) * 3.0
+    z[6, -1] = float(z[6, -1]) + 20.0
+    z[7] = -torch.arange(vocab) // (span // 8) * 3.0
+    z[7, 0] = 20.0
+    z[8, 3], z[9, 4], z[9, vocab // 2] = torch.nan, 30.0, low
+    z = z.to(dt).cuda()
+    fine = [0, 1, 2, 3, 4, 5, 6, 7, 9]
+    at = z.nan_to_num(0.0, posinf=0.0, neginf=low).argmax(1).int()
+    logp, stats, values, columns = _score(torch, z, at, 2, 1.0)
+    assert bool(stats[8].isnan().all()) and bool(logp[8].isnan())
+    want_logp, want = ref.score(z[fine].double(), at[fine], 1.0)
+    log_off, h_off = ref.off(z[fine].double(), 1.0, 16 // z.element_size(), apart=True)
+    err = (stats[fine].double() - want).abs()
+    assert not bool(err[:, 0].any()) and torch.equal(columns[fine, 0], at[fine])
+    assert bool((err[:, 1] <= log_off).all()), (err[:, 1], log_off)
+    assert bool((err[:, 2] <= h_off).all()), (err[:, 2], h_off)
+    assert bool(((logp[fine].double() - want_logp).abs() <= log_off).all())
+    assert torch.equal(values[fine, 0], logp[fine])
