@@ -213,7 +213,8 @@ int zo_i8_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, int
                    const zo_i8 *q, const zo_i8 *qt, void *work, hipStream_t stream);
 
 /* zo_i8_dequantize -- the values of q (scale times code in binary32) into out
- * [q->rows, q->cols]. */
+ * [q->rows, q->cols].  127 times the scale of a row with binary32's largest number, which
+ * is rounded up, passes binary32: it is read back as infinity. */
 int zo_i8_dequantize(const zo_i8 *q, void *out, int32_t dtype, int64_t ld, hipStream_t stream);
 
 /*
@@ -351,10 +352,11 @@ typedef struct zo_score {
  * in one read of the logits.  Where S < 2, S - 1 is formed apart from its 1: log S, the
  * largest log probability and the entropy are then right in relation to themselves, down
  * to terms of 2^-126.  log S and the entropy are not below 0, log p not above.  A d that
- * passes binary32 is -infinity; a difference z - m may pass it.  A row's results are the same bits in any batch and
- * whatever else is wanted.  A logit of -infinity has log p = -infinity and adds 0 to
- * the entropy.  A row of only -infinity has the statistics -infinity, -infinity, 0 and
- * log probabilities of -infinity; in one with a NaN or +infinity all of them are NaN.
+ * passes binary32 is -infinity; a difference z - m may pass it.  A row's results are the
+ * same bits in any batch and whatever else is wanted.  A logit of -infinity has log p =
+ * -infinity and adds 0 to the entropy.  A row of only -infinity has the statistics
+ * -infinity, -infinity, 0 and log probabilities of -infinity; in one with a NaN or
+ * +infinity all of them are NaN.
  */
 int zo_token_logprobs(const zo_score *args, hipStream_t stream);
 

@@ -70,7 +70,10 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t *s)
 // both round to the same whole number the quotient, which lies between, does too; where not,
 // it is near the border of two codes, and a division in 64 bits decides: a quotient of two
 // 24-bit numbers that is not such a border itself is at least 2^-33 of it away, so the rounded
-// 64-bit quotient stands on the same side.  Steps below 2^-100, whose inverse may pass
+// 64-bit quotient stands on the same side.  That is one element in 2^16 of normal values in
+// binary32, 2^11 in binary16 and 2^9 in bfloat16, whose numbers often are half multiples of s (then
+// in 29% of a wave's groups of four: 8192 x 1600 by rows 11.4 us, with a few large columns that
+// make the other codes small 9.1).  Steps below 2^-100, whose inverse may pass
 // binary32, take the division throughout.  Where both inverses are 0 all codes are 0.
 struct Step {
     float s, above, below;

@@ -65,7 +65,9 @@ hipError_t launch_i8_product(const I8View &a, const I8View &b, void *out, int gt
                              hipStream_t st);
 // As for the 4-bit products.  Few rows / tiles, us (rows x matrix): 32 x 6400 x 1600 6.6 / 7.0,
 // 40 8.0 / 7.1; 32 x 50257 x 1600 19.9 / 18.8, 40 21.4 / 18.9; 32 x 1600 x 6400 10.8 / 16.3, 40
-// 14.1 / 16.3, 64 17.0 / 16.6; 16 x 4096 x 1024 3.6 / 5.0, 40 5.2 / 5.0.
+// 14.1 / 16.3, 64 17.0 / 16.6; 16 x 4096 x 1024 3.6 / 5.0, 40 5.2 / 5.0.  Where they cross goes by
+// the matrix, from below 32 rows (50257 x 1600) to above 40 (1600 x 6400); this one bound for all
+// gives away 6% there and 16% here.
 constexpr int kI8FewRows = 32;
 bool i8_few_fits(int64_t n, int64_t k);
 hipError_t launch_i8_few(const I8View &a, const I8View &b, void *out, int gt, int64_t ld,

@@ -179,9 +179,9 @@ __device__ __forceinline__ void move_base(float from, float to, const Slope &by,
 // log probability is above 0.  About each lane's own first vector a base would move with most of
 // a wave's vectors; beyond the first 1024 hardly any holds a larger one.
 //
-// Every N-th of a lane's vectors belongs to the same group, four groups a thread.  The groups' maxima bound the k-th
-// largest logit from below, and only those that reach the bound, few more than are wanted, are
-// read again for the candidates.
+// Every N-th of a lane's vectors belongs to the same group, four groups a thread.  The groups'
+// maxima bound the k-th largest logit from below, and only those that reach the bound, few more
+// than are wanted, are read again for the candidates.
 //
 // Nothing of the row stays in the registers, so that a CU has 2048 threads with several loads
 // each under way: 4096 x 50304 bfloat16 without alternatives 81 us, with 20 104; with the row in
@@ -336,8 +336,8 @@ __global__ __launch_bounds__(TH, 8) void k_score(zo_score a)
 }
 
 // 1024 vectors at most are one for each lane.  Of long rows, four workgroups of 512 threads a
-// CU, or, where a CU has no more than two rows, of 1024: 4096 x 50304 bfloat16, 20 wanted, 106 us
-// against 122; 3 x 50257 binary32, 5 wanted, 12.8 against 10.6.  More wanted logits need the
+// CU, or, where a CU has no more than two rows, of 1024: 4096 x 50304 bfloat16, 20 wanted, 104 us
+// against 123; 3 x 50257 binary32, 5 wanted, 12.8 against 10.6.  More wanted logits need the
 // groups of 1024 threads.
 static hipError_t launch_rows(const zo_score &a, int gt, hipStream_t st)
 {
